@@ -42,7 +42,7 @@ extern "C" {
 typedef enum {
     KLA_OK = 0,
     KLA_ERR_NULL = -1,      /* a required pointer is NULL                                  */
-    KLA_ERR_SHAPE = -2,     /* unsupported or inconsistent B/T/H/d_k/d_v/n_seq             */
+    KLA_ERR_SHAPE = -2,     /* unsupported or inconsistent B/T/H/d_k/d_v/n_seq, channels   */
     KLA_ERR_DTYPE = -3,     /* io_dtype / out_dtype not one of kla_dtype                   */
     KLA_ERR_ALIGN = -4,     /* a pointer is not 16-byte aligned                            */
     KLA_ERR_CHUNK = -5,     /* chunk not in {16, 32, 64}                                   */
@@ -102,6 +102,9 @@ typedef enum { KLA_F32 = 0, KLA_BF16 = 1 } kla_dtype;
 #define KLA_FLAG_NO_SEGMENTS 2            /* never cut sequences into segments                              */
 #define KLA_FLAG_EXACT_SEGMENTS 128       /* segments always from chained transition maps, never from warm-up runs */
 #define KLA_FLAG_SEGMENTS(g) ((g) << 8)   /* force g segments per sequence, 2 <= g <= 255 (fewer if T is short) */
+/* Operators around a mixer (below). */
+#define KLA_FLAG_CONV_LINEAR (1 << 16)    /* kla_conv_*: no activation behind the convolution                */
+#define KLA_FLAG_GATE_FIRST (1 << 17)     /* kla_norm_*: the gate acts before the norm, not behind it         */
 
 typedef struct {
     int32_t B;        /* sequences in the batch; packed (varlen) input: 1                       */
@@ -307,6 +310,87 @@ kla_status kla_bwd(const kla_desc *desc, const void *q, const void *k, const voi
                    const float *log_alpha, const float *eta, float eps, const float *init_state,
                    const void *d_out, const float *d_final_state,
                    float *dq, float *dk, float *dv, float *dlog_alpha, float *deta, float *dinit_state);
+
+/*
+ * ---- Operators around a mixer ------------------------------------------------------------------------------------
+ *
+ * What a layer puts before, beside and behind the mixers above.  Sequences, dtypes, workspace, status word and stream are those of
+ * kla_desc; each call names its own channel counts.  "Rows" are tokens: row b T + t, or the packed tokens.  Inputs whose call takes a
+ * stride may be slices of wider arrays: consecutive rows `stride` elements apart, the elements of a row dense; everything else
+ * is dense.  Pointers 16-byte aligned, those of weight, bias, scale, dt, a and d_skip 4-byte.  Outputs must not overlap inputs except where said.  Sums, states and norms are fp32.
+ *
+ * Short causal depthwise convolution with SiLU:
+ *
+ *     p_t[c] = bias[c] + sum_{i < taps} weight[c][i] x_{t - taps + 1 + i}[c],     y_t = p_t / (1 + exp(-p_t))
+ *
+ * (KLA_FLAG_CONV_LINEAR: y_t = p_t).  Inputs before a sequence's first token are rows of its state, oldest first, or zeros.
+ *   desc: B, T, n_seq, cu_seqlens, host_seqlens, io_dtype, flags, stream are used
+ *   x [rows, channels] io_dtype; 2 <= taps <= 4; weight [channels, taps], bias [channels] (or NULL) fp32
+ *   init_state, final_state [n_seq, taps - 1, channels] io_dtype, or NULL; an input is stored as it is
+ *   out [rows, channels] io_dtype
+ * kla_conv_step: one token per sequence (desc->T 1, no cu_seqlens); x, out [B, channels]; the state moves on by one row in place.
+ * kla_conv_bwd: d_out, dx [rows, channels] io_dtype; d_final_state, dinit_state as the states, or NULL; dweight [channels, taps], dbias
+ *   [channels] (or NULL) fp32, summed in an order that does not vary.  Workspace of kla_conv_bwd_workspace_bytes.
+ */
+kla_status kla_conv_fwd(const kla_desc *desc, int32_t channels, int32_t taps, const void *x, int64_t x_stride,
+                        const float *weight, const float *bias, const void *init_state, void *out, void *final_state);
+kla_status kla_conv_step(const kla_desc *desc, int32_t channels, int32_t taps, const void *x, int64_t x_stride,
+                         const float *weight, const float *bias, void *state_inout, void *out);
+size_t kla_conv_bwd_workspace_bytes(const kla_desc *desc, int32_t channels, int32_t taps);
+kla_status kla_conv_bwd(const kla_desc *desc, int32_t channels, int32_t taps, const void *x, int64_t x_stride,
+                        const float *weight, const float *bias, const void *init_state, const void *d_out,
+                        const void *d_final_state, void *dx, float *dweight, float *dbias, void *dinit_state);
+
+/*
+ * Selective state space scan, the other recurrence over a d_k x d_v state with one decay per token and head:
+ *
+ *     S_t = exp(dt_t a) S_{t-1} + dt_t k_t v_t^T,     o_t = S_t^T q_t + d_skip v_t
+ *
+ * q and k are shared by the H / groups heads of a group (head h: group h / (H / groups)); a and d_skip are per head.  dt > 0 and
+ * a < 0 are meant (a growing state is computed as long as it stays finite), the caller's parametrisation is its own.
+ *   desc: B, T, H, d_k, d_v (multiples of 8 up to 256), n_seq, cu_seqlens, host_seqlens, io_dtype, out_dtype, flags, workspace,
+ *     status_word and stream are used
+ *   q, k [rows, groups, d_k], v [rows, H, d_v] io_dtype, row strides multiples of 16 bytes;  dt [rows, H], a [H], d_skip [H] (or NULL) fp32
+ *   init_state, final_state [n_seq, H, d_k, d_v] fp32 or NULL; out [rows, H, d_v] out_dtype
+ * kla_ssm_step: one token per sequence (desc->T 1, no cu_seqlens), the state updated in place.
+ * kla_ssm_bwd: d_out [rows, H, d_v] io_dtype; d_final_state, dinit_state as the states or NULL; dq, dk [rows, groups, d_k], dv [rows, H,
+ *   d_v] io_dtype, dense; ddt [rows, H], da [H], dd [H] (or NULL) fp32.  The states are recomputed.
+ */
+size_t kla_ssm_fwd_workspace_bytes(const kla_desc *desc, int32_t groups);
+kla_status kla_ssm_fwd(const kla_desc *desc, int32_t groups, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                       const void *v, int64_t v_stride, const float *dt, const float *a, const float *d_skip,
+                       const float *init_state, void *out, float *final_state);
+kla_status kla_ssm_step(const kla_desc *desc, int32_t groups, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                        const void *v, int64_t v_stride, const float *dt, const float *a, const float *d_skip,
+                        float *state_inout, void *out);
+size_t kla_ssm_bwd_workspace_bytes(const kla_desc *desc, int32_t groups);
+kla_status kla_ssm_bwd(const kla_desc *desc, int32_t groups, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                       const void *v, int64_t v_stride, const float *dt, const float *a, const float *d_skip,
+                       const float *init_state, const void *d_out, const float *d_final_state, void *dq, void *dk, void *dv,
+                       float *ddt, float *da, float *dd, float *dinit_state);
+
+/*
+ * RMS norms of a block's input and of a mixer's output, over groups of `group` channels (group = width: the whole row):
+ *
+ *     before a block   u = residual + scale o x (stored in residual_out),   y = norm(u) o weight
+ *     behind a mixer   y = norm(x) o weight o silu(gate),   or, with KLA_FLAG_GATE_FIRST, y = norm(x o silu(gate)) o weight
+ *     plain            y = norm(x) o weight                                  norm(u) = u / sqrt(mean over the group of u^2 + eps)
+ *
+ *   desc: B, T (rows B T), io_dtype, flags, workspace and stream are used
+ *   x, gate, out [rows, width] io_dtype; residual, residual_out [rows, width] fp32 or io_dtype (residual_dtype), both or neither;
+ *   residual_out may be the residual itself; scale [width] (or NULL: 1; needs a residual), weight [width] fp32; a gate and a
+ *   residual exclude each other (KLA_ERR_SHAPE).  The norm is of the sum before it is rounded to residual_out.
+ * kla_norm_bwd takes the forward's inputs: d_out [rows, width] io_dtype; d_residual_out (dtype of the residual, or NULL for zeros) is
+ *   dL/dresidual_out; dx, dgate io_dtype, dresidual (dtype of the residual), dweight, dscale [width] fp32 (dscale may be NULL).
+ */
+kla_status kla_norm_fwd(const kla_desc *desc, int32_t width, int32_t group, const void *x, int64_t x_stride, const void *residual,
+                        int32_t residual_dtype, const float *scale, const void *gate, int64_t gate_stride, const float *weight,
+                        float eps, void *out, void *residual_out);
+size_t kla_norm_bwd_workspace_bytes(const kla_desc *desc, int32_t width, int32_t group);
+kla_status kla_norm_bwd(const kla_desc *desc, int32_t width, int32_t group, const void *x, int64_t x_stride, const void *residual,
+                        int32_t residual_dtype, const float *scale, const void *gate, int64_t gate_stride, const float *weight,
+                        float eps, const void *d_out, const void *d_residual_out, void *dx, void *dresidual, float *dscale,
+                        void *dgate, float *dweight);
 
 /* Static, NUL-terminated description of a status code. */
 const char *kla_status_str(kla_status s);

@@ -17,6 +17,7 @@ KLA_F32, KLA_BF16 = 0, 1
 KLA_FLAG_NONE, KLA_FLAG_FORCE_SIMT, KLA_FLAG_NO_SEGMENTS = 0, 1, 2
 KLA_FLAG_COEFF_ETA, KLA_FLAG_QNORM, KLA_INTERNAL_FLAG_TEST_TIMEOUT, KLA_FLAG_NO_PAIR, KLA_FLAG_WY_FORM = 4, 8, 16, 32, 64
 KLA_FLAG_EXACT_SEGMENTS = 128
+KLA_FLAG_CONV_LINEAR, KLA_FLAG_GATE_FIRST = 1 << 16, 1 << 17
 
 
 def KLA_FLAG_SEGMENTS(g: int) -> int:
@@ -26,7 +27,8 @@ def KLA_FLAG_SEGMENTS(g: int) -> int:
 
 EXPORTS = ["kla_chunk_fwd_workspace_bytes", "kla_chunk_fwd_plan_word_offset", "kla_chunk_fwd", "kla_chunk_fwd_timed", "kla_chunk_fwd_static_scratch",
            "kla_chunk_span_map_workspace_bytes", "kla_chunk_span_map", "kla_state_chain", "kla_dg_fwd", "kla_dg_decode_step", "kla_bwd_workspace_bytes", "kla_bwd", "kla_decode_step", "kla_decode_steps",
-           "kla_status_str", "kla_launch_count"]
+           "kla_conv_fwd", "kla_conv_step", "kla_conv_bwd_workspace_bytes", "kla_conv_bwd", "kla_ssm_fwd_workspace_bytes", "kla_ssm_fwd", "kla_ssm_step",
+           "kla_ssm_bwd_workspace_bytes", "kla_ssm_bwd", "kla_norm_fwd", "kla_norm_bwd_workspace_bytes", "kla_norm_bwd", "kla_status_str", "kla_launch_count"]
 
 
 class KlaError(RuntimeError):
@@ -86,6 +88,16 @@ def load():
     lib.kla_bwd.argtypes = [dp, vp, vp, vp, fp, fp, ctypes.c_float, fp, vp, fp] + [fp] * 6
     lib.kla_decode_steps.restype = ctypes.c_int
     lib.kla_decode_steps.argtypes = [dp, ctypes.c_int32, vp, vp, vp, fp, fp, ctypes.c_float, fp, vp]
+    i32, i64, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    conv, rows3 = [dp, i32, i32, vp, i64, fp, fp], [dp, i32, vp, i64, vp, i64, vp, i64, fp, fp, fp]
+    norm = [dp, i32, i32, vp, i64, vp, i32, fp, vp, i64, fp, ctypes.c_float]
+    for name, res, args in (("kla_conv_fwd", ctypes.c_int, conv + [vp] * 3), ("kla_conv_step", ctypes.c_int, conv + [vp] * 2),
+                            ("kla_conv_bwd_workspace_bytes", sz, [dp, i32, i32]), ("kla_conv_bwd", ctypes.c_int, conv + [vp] * 4 + [fp] * 2 + [vp]),
+                            ("kla_ssm_fwd_workspace_bytes", sz, [dp, i32]), ("kla_ssm_fwd", ctypes.c_int, rows3 + [fp, vp, fp]),
+                            ("kla_ssm_step", ctypes.c_int, rows3 + [fp, vp]), ("kla_ssm_bwd_workspace_bytes", sz, [dp, i32]),
+                            ("kla_ssm_bwd", ctypes.c_int, rows3 + [fp, vp, fp] + [vp] * 3 + [fp] * 4), ("kla_norm_fwd", ctypes.c_int, norm + [vp] * 2),
+                            ("kla_norm_bwd_workspace_bytes", sz, [dp, i32, i32]), ("kla_norm_bwd", ctypes.c_int, norm + [vp] * 4 + [fp, vp, fp])):
+        getattr(lib, name).restype, getattr(lib, name).argtypes = res, args
     lib.kla_status_str.restype = ctypes.c_char_p
     lib.kla_status_str.argtypes = [ctypes.c_int]
     lib.kla_launch_count.restype = ctypes.c_uint64
@@ -370,3 +382,87 @@ def kla_dg_decode_step(q, k, v, log_alpha, eta, eps, state_inout, out=None, out_
     if _host is None:
         load()
     return _host.decode(q, k, v, log_alpha, eta, eps, state_inout, out, out_dtype, flags, 2)
+
+
+# ---- operators around a mixer (include/kla.h) -------------------------------------------------------------------------------------
+# CUDA tensors of one device.  x, q, k, v and gate may be slices of wider arrays as long as a row's elements are dense and the rows lie at one
+# distance from each other; everything else is contiguous.  Outputs are allocated unless passed in.
+
+def kla_conv_fwd(x, weight, bias=None, init_state=None, out=None, final_state=None, cu_seqlens=None, host_seqlens=None, flags=KLA_FLAG_NONE,
+                 want_final_state=True):
+    """Short causal depthwise convolution with SiLU (include/kla.h: kla_conv_fwd).  x [B, T, C] fp32 or bf16; weight [C, taps], 2 to 4 taps, and
+    bias [C] fp32; init_state, final_state [n_seq, taps - 1, C] in x's dtype: the inputs before the first and up to the last token.
+    Packed input as kla_chunk_fwd.  KLA_FLAG_CONV_LINEAR: no SiLU.  Returns (out, final_state)."""
+    if _host is None:
+        load()
+    if cu_seqlens is not None and host_seqlens is None:
+        host_seqlens = cu_seqlens.cpu()
+    return _host.conv_fwd(x, weight, bias, init_state, out, final_state, cu_seqlens, host_seqlens, flags, want_final_state)
+
+
+def kla_conv_step(x, weight, state_inout, bias=None, out=None, flags=KLA_FLAG_NONE):
+    """One token of the convolution for each of B sequences (include/kla.h: kla_conv_step): x [B, C]; state_inout [B, taps - 1, C] moves on
+    in place.  Returns out [B, C]."""
+    if _host is None:
+        load()
+    return _host.conv_step(x, weight, state_inout, bias, out, flags)
+
+
+def kla_conv_bwd(x, weight, d_out, bias=None, init_state=None, d_final_state=None, cu_seqlens=None, host_seqlens=None, flags=KLA_FLAG_NONE,
+                 want_dinit_state=True):
+    """Gradients of kla_conv_fwd given d_out [B, T, C] and d_final_state (or None): dict of dx and dinit_state in x's dtype, dweight and dbias
+    in fp32 (dbias None without a bias, dinit_state None unless asked for)."""
+    if _host is None:
+        load()
+    if cu_seqlens is not None and host_seqlens is None:
+        host_seqlens = cu_seqlens.cpu()
+    return _host.conv_bwd(x, weight, d_out, bias, init_state, d_final_state, cu_seqlens, host_seqlens, flags, want_dinit_state)
+
+
+def kla_ssm_fwd(q, k, v, dt, a, d_skip=None, init_state=None, out=None, final_state=None, cu_seqlens=None, host_seqlens=None, out_dtype=None,
+                flags=KLA_FLAG_NONE, want_final_state=True, status_word=None):
+    """Selective state space scan (include/kla.h: kla_ssm_fwd): S_t = exp(dt_t a) S + dt_t k_t v_t^T, o_t = S_t^T q_t + d_skip v_t.
+    q, k [B, T, G, d_k], v [B, T, H, d_v] fp32 or bf16, each group's q and k serving H / G heads; dt [B, T, H], a [H], d_skip [H] fp32;
+    states [n_seq, H, d_k, d_v] fp32.  Packed input, out_dtype and `status_word` as kla_chunk_fwd.  Returns (out, final_state)."""
+    if _host is None:
+        load()
+    if cu_seqlens is not None and host_seqlens is None:
+        host_seqlens = cu_seqlens.cpu()
+    return _host.ssm_fwd(q, k, v, dt, a, d_skip, init_state, out, final_state, cu_seqlens, host_seqlens, out_dtype, flags, want_final_state, status_word)
+
+
+def kla_ssm_step(q, k, v, dt, a, state_inout, d_skip=None, out=None, out_dtype=None, flags=KLA_FLAG_NONE):
+    """One token of the scan for each of B sequences (include/kla.h: kla_ssm_step): q, k [B, G, d_k]; v [B, H, d_v]; dt [B, H]; state_inout
+    [B, H, d_k, d_v] fp32, updated in place.  Returns out [B, H, d_v]."""
+    if _host is None:
+        load()
+    return _host.ssm_step(q, k, v, dt, a, state_inout, d_skip, out, out_dtype, flags)
+
+
+def kla_ssm_bwd(q, k, v, dt, a, d_out, d_skip=None, init_state=None, d_final_state=None, cu_seqlens=None, host_seqlens=None, flags=KLA_FLAG_NONE,
+                want_dinit_state=True, status_word=None):
+    """Gradients of kla_ssm_fwd given d_out (dtype of v) and d_final_state (or None): dict of dq, dk, dv in the inputs' dtype and ddt, da, dd,
+    dinit_state in fp32 (dd None without d_skip, dinit_state None unless asked for)."""
+    if _host is None:
+        load()
+    if cu_seqlens is not None and host_seqlens is None:
+        host_seqlens = cu_seqlens.cpu()
+    return _host.ssm_bwd(q, k, v, dt, a, d_out, d_skip, init_state, d_final_state, cu_seqlens, host_seqlens, flags, want_dinit_state, status_word)
+
+
+def kla_norm_fwd(x, weight, eps, residual=None, scale=None, gate=None, group=None, out=None, residual_out=None, flags=KLA_FLAG_NONE):
+    """RMS norm of a block's input or of a mixer's output (include/kla.h: kla_norm_fwd), x [..., width] fp32 or bf16, weight [width] fp32, over
+    groups of `group` channels (default: the row).  With a residual (fp32 or x's dtype): of u = residual + scale o x, which is returned
+    too (residual_out may be the residual itself); with a gate: times silu(gate) behind the norm, or before it with
+    KLA_FLAG_GATE_FIRST.  Returns (out, residual_out or None)."""
+    if _host is None:
+        load()
+    return _host.norm_fwd(x, weight, eps, residual, scale, gate, group, out, residual_out, flags)
+
+
+def kla_norm_bwd(x, weight, eps, d_out, residual=None, scale=None, gate=None, group=None, d_residual_out=None, flags=KLA_FLAG_NONE):
+    """Gradients of kla_norm_fwd from its inputs, d_out and (with a residual) d_residual_out or None: dict of dx, dgate in x's dtype, dresidual
+    in the residual's, dweight and dscale in fp32; None for what the call was not given."""
+    if _host is None:
+        load()
+    return _host.norm_bwd(x, weight, eps, d_out, residual, scale, gate, group, d_residual_out, flags)

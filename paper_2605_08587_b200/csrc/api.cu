@@ -19,7 +19,7 @@ int sm_count()
 
 static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-static kla_status check_arch()
+kla_status check_arch()
 {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return KLA_ERR_ARCH;   // (no usable device: there is no fallback)

@@ -1,0 +1,433 @@
+// Short causal depthwise convolution over packed or fixed-length sequences, with SiLU: forward, backward and one token.
+//
+//   p_t[c] = b[c] + sum_{i < W} w[c][i] x_{t-W+1+i}[c]     (inputs before a sequence's first token: its state, else zeros)
+//   y_t = p_t sigmoid(p_t)                                  (KLA_FLAG_CONV_LINEAR: y_t = p_t)
+//
+// Backward, with g_t = dy_t act'(p_t):   dx_t = sum_i w[i] g_{t+W-1-i} (tokens of the same sequence), plus the final state's gradient
+// for the last W - 1 tokens;  dw[c][i] = sum_t g_t x_{t-W+1+i};  db = sum_t g_t.
+//
+// Memory-bound: W multiply-adds and one exponential per value.  A thread owns a few neighbouring channels and walks a run of tokens
+// with the window in registers, so a value is loaded once, but for the W - 1 before (backward: and behind) its run.
+#include "layer_ops.h"
+#include "layer_pieces.cuh"
+
+namespace kla {
+
+template <typename IO, int VEC>
+__device__ __forceinline__ void load_or_zero(Pack<IO, VEC> &x, const IO *p)
+{
+    if (p) x.load(p);
+    else x.zero();
+}
+
+// Row `pos` of a sequence as the window sees it: pos >= 0 a token, pos < 0 a row of its state.
+template <typename IO, int VEC>
+__device__ __forceinline__ void window_row(Pack<IO, VEC> &x, const ConvParams &p, int seq, int start, int pos, int c)
+{
+    const IO *init = static_cast<const IO *>(p.init_state);
+    const int W1 = p.taps - 1;
+    load_or_zero(x, pos >= 0 ? static_cast<const IO *>(p.x) + (size_t)(start + pos) * p.x_stride + c
+                   : init    ? init + ((size_t)seq * W1 + W1 + pos) * p.C + c
+                             : nullptr);
+}
+
+// Units of work: (run of tokens, VEC channels), then, where a final state is wanted, (sequence, VEC channels).
+template <typename IO, int W, int VEC, bool SILU>
+__global__ void __launch_bounds__(256) conv_fwd_kernel(ConvParams p, Sequences seqs, int run, int n_runs)
+{
+    const int nvec = p.C / VEC;
+    const long long unit = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int c = (int)(unit % nvec) * VEC;
+    const long long job = unit / nvec;
+    if (job >= n_runs) {   // final states: the last W - 1 rows of the window, whatever a sequence's length
+        const long long n = job - n_runs;
+        if (!p.final_state || n >= p.n_seq) return;
+        const int start = seqs.start((int)n), len = seqs.start((int)n + 1) - start;
+        Pack<IO, VEC> x;
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) {
+            window_row<IO, VEC>(x, p, (int)n, start, len - (W - 1) + i, c);
+            x.store(static_cast<IO *>(p.final_state) + ((size_t)n * (W - 1) + i) * p.C + c);
+        }
+        return;
+    }
+    const int r0 = (int)job * run, r1 = min(p.rows, r0 + run);
+    float w[W][VEC], b[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        b[e] = p.bias ? p.bias[c + e] : 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i][e] = p.weight[(size_t)(c + e) * W + i];
+    }
+    int seq = seqs.of_row(r0), start = seqs.start(seq), end = seqs.start(seq + 1);
+    float win[W - 1][VEC];
+    auto fill = [&](int pos) {   // the window before token `pos`
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) {
+            Pack<IO, VEC> x;
+            window_row<IO, VEC>(x, p, seq, start, pos - (W - 1) + i, c);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) win[i][e] = x.get(e);
+        }
+    };
+    fill(r0 - start);
+    const IO *xp = static_cast<const IO *>(p.x) + c;
+    IO *yp = static_cast<IO *>(p.out) + c;
+    constexpr int AHEAD = 8;   // rows in flight
+    for (int r = r0; r < r1; r += AHEAD) {
+        Pack<IO, VEC> raw[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (r + j < r1) raw[j].load(xp + (size_t)(r + j) * p.x_stride);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (r + j >= r1) break;
+            if (r + j == end) {
+                do {
+                    ++seq;
+                    start = end;
+                    end = seqs.start(seq + 1);
+                } while (end == start && seq + 1 < p.n_seq);
+                fill(0);
+            }
+            float y[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float x = raw[j].get(e);
+                float s = b[e];
+#pragma unroll
+                for (int i = 0; i < W - 1; ++i) s = fmaf(w[i][e], win[i][e], s);
+                s = fmaf(w[W - 1][e], x, s);
+                y[e] = SILU ? s * sigmoid(s) : s;
+#pragma unroll
+                for (int i = 0; i + 1 < W - 1; ++i) win[i][e] = win[i + 1][e];
+                win[W - 2][e] = x;
+            }
+            Pack<IO, VEC> o;
+            o.set(y);
+            o.store(yp + (size_t)(r + j) * p.C);
+        }
+    }
+}
+
+// One thread: VEC channels of one sequence's next token; the window moves on by one row.
+template <typename IO, int W, int VEC, bool SILU>
+__global__ void __launch_bounds__(128) conv_step_kernel(ConvParams p)
+{
+    const int nvec = p.C / VEC;
+    const long long unit = (long long)blockIdx.x * 128 + threadIdx.x;
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // what the previous kernel on the stream wrote may be read here
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (unit >= (long long)p.rows * nvec) return;
+    const int c = (int)(unit % nvec) * VEC;
+    const size_t n = (size_t)(unit / nvec);
+    IO *state = static_cast<IO *>(p.final_state) + n * (W - 1) * p.C + c;
+    Pack<IO, VEC> x[W];
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) x[i].load(state + (size_t)i * p.C);
+    x[W - 1].load(static_cast<const IO *>(p.x) + n * p.x_stride + c);
+    float y[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        float s = p.bias ? p.bias[c + e] : 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) s = fmaf(p.weight[(size_t)(c + e) * W + i], x[i].get(e), s);
+        y[e] = SILU ? s * sigmoid(s) : s;
+    }
+    Pack<IO, VEC> o;
+    o.set(y);
+    o.store(static_cast<IO *>(p.out) + n * p.C + c);
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) x[i + 1].store(state + (size_t)i * p.C);
+}
+
+// A block: 32 x VEC channels and the rows [y rows_per, ..), an eighth of them to each of its warps.  The sums over rows stay in registers,
+// then the warps' are added in shared memory and leave as one partial of [W + 1][C] per block row; conv_reduce_kernel adds those in order.
+template <typename IO, int W, int VEC, bool SILU>
+__global__ void __launch_bounds__(256) conv_bwd_kernel(ConvParams p, Sequences seqs, int rows_per)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = (blockIdx.x * 32 + lane) * VEC;
+    const int b0 = blockIdx.y * rows_per, b1 = min(p.rows, b0 + rows_per);
+    const int sub = (rows_per + 7) / 8;
+    const int r0 = min(b1, b0 + warp * sub), r1 = min(b1, r0 + sub);
+    float dw[W][VEC], db[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        db[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) dw[i][e] = 0.f;
+    }
+    if (r0 < r1 && c < p.C) {
+        float w[W][VEC], b[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            b[e] = p.bias ? p.bias[c + e] : 0.f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i][e] = p.weight[(size_t)(c + e) * W + i];
+        }
+        int seq = seqs.of_row(r0), start = seqs.start(seq), end = seqs.start(seq + 1);
+        float win[W - 1][VEC], acc[W][VEC];   // acc[s]: gradient of row t - s so far
+        auto fill = [&](int pos) {
+#pragma unroll
+            for (int i = 0; i < W - 1; ++i) {
+                Pack<IO, VEC> x;
+                window_row<IO, VEC>(x, p, seq, start, pos - (W - 1) + i, c);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) win[i][e] = x.get(e);
+            }
+        };
+        fill(r0 - start);
+#pragma unroll
+        for (int s = 0; s < W; ++s)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) acc[s][e] = 0.f;
+        const IO *xp = static_cast<const IO *>(p.x) + c, *gp = static_cast<const IO *>(p.d_out) + c, *fp = static_cast<const IO *>(p.d_final);
+        IO *dxp = static_cast<IO *>(p.dx) + c;
+        const int last = r1 + W - 1;   // the rows behind the run whose windows reach into it
+        constexpr int AHEAD = 4;
+        for (int t0 = r0; t0 < last; t0 += AHEAD) {
+            Pack<IO, VEC> xr[AHEAD], gr[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+                if (t0 + j < last && t0 + j < p.rows) {
+                    xr[j].load(xp + (size_t)(t0 + j) * p.x_stride);
+                    gr[j].load(gp + (size_t)(t0 + j) * p.C);
+                }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                const int t = t0 + j;
+                if (t >= last) break;
+#pragma unroll
+                for (int s = W - 1; s > 0; --s)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) acc[s][e] = acc[s - 1][e];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) acc[0][e] = 0.f;
+                if (t < p.rows) {
+                    if (t == end) {
+                        do {
+                            ++seq;
+                            start = end;
+                            end = seqs.start(seq + 1);
+                        } while (end == start && seq + 1 < p.n_seq);
+                        fill(0);
+                    }
+                    if (fp && t >= end - (W - 1)) {
+                        Pack<IO, VEC> f;
+                        f.load(fp + ((size_t)seq * (W - 1) + (t - (end - (W - 1)))) * p.C + c);
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) acc[0][e] = f.get(e);
+                    }
+                    const int pos = t - start;
+                    const bool mine = t < r1;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const float x = xr[j].get(e);
+                        float g = gr[j].get(e);
+                        if (SILU) {
+                            float s = b[e];
+#pragma unroll
+                            for (int i = 0; i < W - 1; ++i) s = fmaf(w[i][e], win[i][e], s);
+                            s = fmaf(w[W - 1][e], x, s);
+                            const float sig = sigmoid(s);
+                            g *= sig * fmaf(s, 1.f - sig, 1.f);
+                        }
+                        if (mine) {
+                            db[e] += g;
+#pragma unroll
+                            for (int i = 0; i < W - 1; ++i) dw[i][e] = fmaf(g, win[i][e], dw[i][e]);
+                            dw[W - 1][e] = fmaf(g, x, dw[W - 1][e]);
+                        }
+#pragma unroll
+                        for (int s = 0; s < W; ++s)
+                            if (s <= pos) acc[s][e] = fmaf(w[W - 1 - s][e], g, acc[s][e]);
+#pragma unroll
+                        for (int i = 0; i + 1 < W - 1; ++i) win[i][e] = win[i + 1][e];
+                        win[W - 2][e] = x;
+                    }
+                }
+                const int done = t - (W - 1);   // (below r1: t is below r1 + W - 1)
+                if (done >= r0) {
+                    Pack<IO, VEC> o;
+                    o.set(acc[W - 1]);
+                    o.store(dxp + (size_t)done * p.C);
+                }
+            }
+        }
+    }
+    __shared__ float sums[8][32 * VEC];
+#pragma unroll
+    for (int i = 0; i <= W; ++i) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sums[warp][lane * VEC + e] = i < W ? dw[i < W ? i : 0][e] : db[e];
+        __syncthreads();
+        for (int x = threadIdx.x; x < 32 * VEC; x += 256) {
+            const int ch = blockIdx.x * 32 * VEC + x;
+            if (ch < p.C) {
+                float s = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s += sums[k][x];
+                p.partial[((size_t)blockIdx.y * (W + 1) + i) * p.C + ch] = s;
+            }
+        }
+    }
+}
+
+__global__ void __launch_bounds__(512) conv_reduce_kernel(const float *partial, int n, int W, int C, float *dweight, float *dbias)
+{
+    sum_partials(partial, n, (W + 1) * C, [&](int i, float s) {
+        const int tap = i / C, c = i % C;
+        if (tap < W) dweight[(size_t)c * W + tap] = s;
+        else if (dbias) dbias[c] = s;
+    });
+}
+
+// Gradient of the states: one thread per (sequence, channel); the first W - 1 tokens' windows reach into the state, and in a sequence
+// shorter than that the final state's gradient does too.
+template <typename IO, int W, bool SILU>
+__global__ void __launch_bounds__(256) conv_dinit_kernel(ConvParams p, Sequences seqs)
+{
+    const long long unit = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (unit >= (long long)p.n_seq * p.C) return;
+    const int n = (int)(unit / p.C), c = (int)(unit % p.C);
+    const int start = seqs.start(n), len = seqs.start(n + 1) - start;
+    float d[W - 1];
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j)
+        d[j] = p.d_final && j >= len ? to_f32(static_cast<const IO *>(p.d_final)[((size_t)n * (W - 1) + j - len) * p.C + c]) : 0.f;
+#pragma unroll
+    for (int t = 0; t < W - 1; ++t) {
+        if (t >= len) break;
+        float s = p.bias ? p.bias[c] : 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            Pack<IO, 1> x;
+            window_row<IO, 1>(x, p, n, start, t - (W - 1) + i, c);
+            s = fmaf(p.weight[(size_t)c * W + i], x.get(0), s);
+        }
+        float g = to_f32(static_cast<const IO *>(p.d_out)[(size_t)(start + t) * p.C + c]);
+        if (SILU) {
+            const float sig = sigmoid(s);
+            g *= sig * fmaf(s, 1.f - sig, 1.f);
+        }
+#pragma unroll
+        for (int j = t; j < W - 1; ++j) d[j] = fmaf(p.weight[(size_t)c * W + j - t], g, d[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) static_cast<IO *>(p.dinit)[((size_t)n * (W - 1) + j) * p.C + c] = from_f32<IO>(d[j]);
+}
+
+// ---- launches ---------------------------------------------------------------------------------------------------------------
+static int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+template <typename F>
+static cudaError_t with_taps(int taps, bool silu, F f)
+{
+    using std::integral_constant;
+    switch (taps * 2 + (silu ? 1 : 0)) {
+        case 4: return f(integral_constant<int, 2>(), integral_constant<bool, false>());
+        case 5: return f(integral_constant<int, 2>(), integral_constant<bool, true>());
+        case 6: return f(integral_constant<int, 3>(), integral_constant<bool, false>());
+        case 7: return f(integral_constant<int, 3>(), integral_constant<bool, true>());
+        case 8: return f(integral_constant<int, 4>(), integral_constant<bool, false>());
+        default: return f(integral_constant<int, 4>(), integral_constant<bool, true>());
+    }
+}
+
+template <typename IO, int VEC>
+static cudaError_t conv_fwd_v(const ConvParams &p, cudaStream_t stream)
+{
+    const Sequences seqs = {p.cu_seqlens, p.T, p.n_seq};
+    const int nvec = p.C / VEC;
+    // Runs as long as leave every SM some 1500 threads, 8 to 64 rows: the rows before a run are loaded twice.
+    long long run = (long long)p.rows * nvec / ((long long)sm_count() * 1536) / 8 * 8;
+    run = run < 8 ? 8 : run > 64 ? 64 : run;
+    const int n_runs = ceil_div(p.rows, run);
+    const long long units = ((long long)n_runs + (p.final_state ? p.n_seq : 0)) * nvec;
+    if (units == 0) return cudaSuccess;
+    return with_taps(p.taps, p.silu, [&](auto W, auto SILU) {
+        conv_fwd_kernel<IO, W(), VEC, SILU()><<<ceil_div(units, 256), 256, 0, stream>>>(p, seqs, (int)run, n_runs);
+        count_launch(1);
+        return cudaGetLastError();
+    });
+}
+
+template <typename IO, int VEC>
+static cudaError_t conv_step_v(const ConvParams &p, cudaStream_t stream)
+{
+    const long long units = (long long)p.rows * (p.C / VEC);
+    if (units == 0) return cudaSuccess;
+    return with_taps(p.taps, p.silu, [&](auto W, auto SILU) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)ceil_div(units, 128));
+        cfg.blockDim = dim3(128);
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        const cudaError_t err = cudaLaunchKernelEx(&cfg, conv_step_kernel<IO, W(), VEC, SILU()>, p);
+        count_launch(1);
+        return err != cudaSuccess ? err : cudaGetLastError();
+    });
+}
+
+// Rows of the grid of the backward: enough blocks for four on every SM, none with fewer than 64 rows.
+static int conv_bwd_rows(int C, int vec, int rows)
+{
+    const int cols = ceil_div(C, 32 * vec);
+    int ny = ceil_div(4LL * sm_count(), cols);
+    const int most = ceil_div(rows, 64);
+    return ny < 1 ? 1 : ny > most ? (most < 1 ? 1 : most) : ny;
+}
+
+template <typename IO, int VEC>
+static cudaError_t conv_bwd_v(const ConvParams &p, cudaStream_t stream)
+{
+    const Sequences seqs = {p.cu_seqlens, p.T, p.n_seq};
+    const int ny = conv_bwd_rows(p.C, VEC, p.rows), per = p.rows ? ceil_div(p.rows, ny) : 1;
+    return with_taps(p.taps, p.silu, [&](auto W, auto SILU) {
+        conv_bwd_kernel<IO, W(), VEC, SILU()><<<dim3((unsigned)ceil_div(p.C, 32 * VEC), (unsigned)ny), 256, 0, stream>>>(p, seqs, per);
+        conv_reduce_kernel<<<ceil_div((long long)(W() + 1) * p.C, 32), 512, 0, stream>>>(p.partial, ny, W(), p.C, p.dweight, p.dbias);
+        count_launch(2);
+        if (p.dinit) {
+            conv_dinit_kernel<IO, W(), SILU()><<<ceil_div((long long)p.n_seq * p.C, 256), 256, 0, stream>>>(p, seqs);
+            count_launch(1);
+        }
+        return cudaGetLastError();
+    });
+}
+
+// Channels of a thread: 16 bytes (backward 8: twice the arrays are in registers) where rows start on such a boundary, else one.
+static bool whole_packs(const ConvParams &p, int vec, int io_dtype)
+{
+    const int bytes = io_dtype == KLA_BF16 ? 2 : 4;
+    const size_t to = (size_t)vec * bytes;
+    return p.C % vec == 0 && (size_t)p.x_stride * bytes % to == 0;
+}
+
+size_t conv_bwd_workspace_bytes(int C, int taps, int rows)
+{
+    const int a = conv_bwd_rows(C, 4, rows), b = conv_bwd_rows(C, 1, rows);
+    return (size_t)(a > b ? a : b) * (taps + 1) * C * sizeof(float);
+}
+cudaError_t launch_conv_fwd(const ConvParams &p, int io_dtype, cudaStream_t stream)
+{
+    if (io_dtype == KLA_BF16) return whole_packs(p, 8, io_dtype) ? conv_fwd_v<__nv_bfloat16, 8>(p, stream) : conv_fwd_v<__nv_bfloat16, 1>(p, stream);
+    return whole_packs(p, 4, io_dtype) ? conv_fwd_v<float, 4>(p, stream) : conv_fwd_v<float, 1>(p, stream);
+}
+cudaError_t launch_conv_step(const ConvParams &p, int io_dtype, cudaStream_t stream)
+{
+    if (io_dtype == KLA_BF16) return whole_packs(p, 4, io_dtype) ? conv_step_v<__nv_bfloat16, 4>(p, stream) : conv_step_v<__nv_bfloat16, 1>(p, stream);
+    return whole_packs(p, 4, io_dtype) ? conv_step_v<float, 4>(p, stream) : conv_step_v<float, 1>(p, stream);
+}
+cudaError_t launch_conv_bwd(const ConvParams &p, int io_dtype, cudaStream_t stream)
+{
+    if (io_dtype == KLA_BF16) return whole_packs(p, 4, io_dtype) ? conv_bwd_v<__nv_bfloat16, 4>(p, stream) : conv_bwd_v<__nv_bfloat16, 1>(p, stream);
+    return whole_packs(p, 4, io_dtype) ? conv_bwd_v<float, 4>(p, stream) : conv_bwd_v<float, 1>(p, stream);
+}
+
+}  // namespace kla
