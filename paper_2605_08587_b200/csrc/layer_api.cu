@@ -227,6 +227,8 @@ kla_status kla_ssm_fwd(const kla_desc *desc, int32_t groups, const void *q, int6
     p.init_state = init_state;
     p.out = out;
     p.final_state = final_state;
+    if (ssm_chunk_supported(desc->io_dtype, p.N, p.P, p.rows) && !(desc->flags & KLA_FLAG_FORCE_SIMT))
+        return launched(launch_ssm_chunk(p, desc->out_dtype, (cudaStream_t)desc->stream));
     return launched(launch_ssm_scan(p, desc->io_dtype, desc->out_dtype, (cudaStream_t)desc->stream));
 }
 

@@ -56,7 +56,7 @@ size_t norm_bwd_workspace_bytes(int rows, int width, int group);
 cudaError_t launch_norm_fwd(const NormParams &p, int io_dtype, int res_dtype, cudaStream_t stream);
 cudaError_t launch_norm_bwd(const NormParams &p, int io_dtype, int res_dtype, cudaStream_t stream);
 
-// Selective state space scan: ssm_scan.cu (any sizes, fp32 arithmetic on CUDA cores).
+// Selective state space scan.  ssm_scan.cu: any sizes, fp32 arithmetic on CUDA cores.
 struct SsmParams {
     const void *q, *k;            // [rows, G, N], rows q_stride / k_stride elements apart
     const void *v;                // [rows, H, P], rows v_stride apart
@@ -82,6 +82,9 @@ struct SsmParams {
 };
 cudaError_t launch_ssm_scan(const SsmParams &p, int io_dtype, int out_dtype, cudaStream_t stream);
 cudaError_t launch_ssm_step(const SsmParams &p, int io_dtype, int out_dtype, cudaStream_t stream);
+// The same by chunks on the tensor cores (ssm_chunk.cu): bf16, N 64 or 128, P a multiple of 64.
+bool ssm_chunk_supported(int io_dtype, int N, int P, int rows);
+cudaError_t launch_ssm_chunk(const SsmParams &p, int out_dtype, cudaStream_t stream);
 size_t ssm_bwd_workspace_bytes(int rows, int n_seq, int H, int G, int N, int P);
 cudaError_t launch_ssm_bwd(const SsmParams &p, int io_dtype, cudaStream_t stream);
 
