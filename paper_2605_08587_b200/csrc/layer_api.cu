@@ -101,7 +101,8 @@ static kla_status ssm_args(const kla_desc *d, int32_t groups, const void *q, int
     p->a = a;
     p->skip = d_skip;
     p->cu_seqlens = d->cu_seqlens;
-    p->host_seqlens = d->host_seqlens;
+    p->host_seqlens = d->cu_seqlens ? d->host_seqlens : nullptr;
+    p->whole = (d->flags & KLA_FLAG_NO_SEGMENTS) != 0;
     p->q_stride = q_stride;
     p->k_stride = k_stride;
     p->v_stride = v_stride;
@@ -212,7 +213,33 @@ kla_status kla_conv_bwd(const kla_desc *desc, int32_t channels, int32_t taps, co
     return launched(launch_conv_bwd(p, desc->io_dtype, (cudaStream_t)desc->stream));
 }
 
-size_t kla_ssm_fwd_workspace_bytes(const kla_desc *, int32_t) { return 0; }
+// The sizes alone
+static SsmParams ssm_sizes(const kla_desc *d, int64_t rows, int32_t groups)
+{
+    SsmParams p = {};
+    p.rows = (int32_t)rows;
+    p.T = d->T;
+    p.n_seq = d->n_seq;
+    p.host_seqlens = d->cu_seqlens ? d->host_seqlens : nullptr;
+    p.H = d->H;
+    p.G = groups;
+    p.N = d->d_k;
+    p.P = d->d_v;
+    p.whole = (d->flags & KLA_FLAG_NO_SEGMENTS) != 0;
+    return p;
+}
+static bool on_tensor_cores(const kla_desc *d, const SsmParams &p)
+{
+    return ssm_chunk_supported(d->io_dtype, p.N, p.P, p.rows) && !(d->flags & KLA_FLAG_FORCE_SIMT);
+}
+
+size_t kla_ssm_fwd_workspace_bytes(const kla_desc *desc, int32_t groups)
+{
+    int64_t rows = 0;
+    if (check_rows(desc, &rows) != KLA_OK || check_sequences(desc) != KLA_OK || desc->H < 1 || groups < 1) return 0;
+    const SsmParams p = ssm_sizes(desc, rows, groups);
+    return on_tensor_cores(desc, p) ? ssm_chunk_workspace_bytes(p) : 0;
+}
 
 kla_status kla_ssm_fwd(const kla_desc *desc, int32_t groups, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
                        int64_t v_stride, const float *dt, const float *a, const float *d_skip, const float *init_state, void *out, float *final_state)
@@ -227,8 +254,7 @@ kla_status kla_ssm_fwd(const kla_desc *desc, int32_t groups, const void *q, int6
     p.init_state = init_state;
     p.out = out;
     p.final_state = final_state;
-    if (ssm_chunk_supported(desc->io_dtype, p.N, p.P, p.rows) && !(desc->flags & KLA_FLAG_FORCE_SIMT))
-        return launched(launch_ssm_chunk(p, desc->out_dtype, (cudaStream_t)desc->stream));
+    if (on_tensor_cores(desc, p)) return launched(launch_ssm_chunk(p, desc->out_dtype, (cudaStream_t)desc->stream));
     return launched(launch_ssm_scan(p, desc->io_dtype, desc->out_dtype, (cudaStream_t)desc->stream));
 }
 

@@ -71,6 +71,7 @@ struct SsmParams {
     int32_t rows, T, n_seq, H, G, N, P;
     int32_t *status_word;         // or null
     int32_t test_timeout;
+    int32_t whole;                // sequences are never cut into parts
     void *workspace;
     // backward
     const void *d_out;            // [rows, H, P]
@@ -84,6 +85,7 @@ cudaError_t launch_ssm_scan(const SsmParams &p, int io_dtype, int out_dtype, cud
 cudaError_t launch_ssm_step(const SsmParams &p, int io_dtype, int out_dtype, cudaStream_t stream);
 // The same by chunks on the tensor cores (ssm_chunk.cu): bf16, N 64 or 128, P a multiple of 64.
 bool ssm_chunk_supported(int io_dtype, int N, int P, int rows);
+size_t ssm_chunk_workspace_bytes(const SsmParams &p);
 cudaError_t launch_ssm_chunk(const SsmParams &p, int out_dtype, cudaStream_t stream);
 size_t ssm_bwd_workspace_bytes(int rows, int n_seq, int H, int G, int N, int P);
 cudaError_t launch_ssm_bwd(const SsmParams &p, int io_dtype, cudaStream_t stream);

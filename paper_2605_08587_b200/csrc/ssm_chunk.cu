@@ -29,7 +29,6 @@
 // head, so that the chain needs no products (the delta rule's segments need whole transition maps).
 #include <mutex>
 
-#include "scan_pieces.cuh"
 #include "ssm_pieces.cuh"
 
 namespace kla {
@@ -89,27 +88,8 @@ static_assert(sizeof(Smem<1>) <= 232448 && sizeof(Smem<2>) <= 232448, "shared me
 
 struct Params {
     SsmParams a;
-    int parts, seg_len;
-    float *part_state;   // [n_seq parts][H][N][P]: what a part adds (first pass), the state it starts from (main pass)
-    float *part_decay;   // [n_seq parts][H]
+    Parts parts;
 };
-
-// Row r of a tile as stored (16-byte pieces permuted)
-__device__ __forceinline__ uint4 *piece(unsigned char *tile, int r, int c) { return reinterpret_cast<uint4 *>(tile + sw128(r, c)); }
-
-__device__ __forceinline__ float2 unpack2(uint32_t x) { return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
-__device__ __forceinline__ uint32_t pack2(float2 x)
-{
-    const __nv_bfloat162 p = __floats2bfloat162_rn(x.x, x.y);
-    return *reinterpret_cast<const uint32_t *>(&p);
-}
-// The bf16 part of x, which keeps the rest.
-__device__ __forceinline__ uint32_t part(float2 &x)
-{
-    const uint32_t h = pack2(x);
-    x = fma2(unpack2(h), f2(-1.f), x);   // exact
-    return h;
-}
 
 // w v of 64 tokens in three parts, by 256 threads: a thread to a quarter of a token's columns.
 __device__ __forceinline__ void weigh(const unsigned char *x, unsigned char (*w)[TILE], int tokens, const float *weight)
@@ -126,44 +106,6 @@ __device__ __forceinline__ void weigh(const unsigned char *x, unsigned char (*w)
         *reinterpret_cast<uint4 *>(w[2] + at) = make_uint4(pack2(v[0]), pack2(v[1]), pack2(v[2]), pack2(v[3]));
     }
 }
-constexpr int HS = NS / 2;   // columns of the state of a thread: it holds half a row
-// S <- gamma S + (what the chunk adds)
-__device__ __forceinline__ void join(float2 (&S)[HS / 2], uint32_t tm, float gamma)
-{
-    const float2 g = f2(gamma);
-#pragma unroll
-    for (int c = 0; c < HS; c += 16) {
-        float h[16], m[16], l[16];
-        tmem_ld16(tm + c, h);
-        tmem_ld16(tm + 64 + c, m);
-        tmem_ld16(tm + 128 + c, l);
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-            const float2 sum = add2(add2(f2(l[e], l[e + 1]), f2(m[e], m[e + 1])), f2(h[e], h[e + 1]));
-            S[(c + e) / 2] = fma2(g, S[(c + e) / 2], sum);
-        }
-    }
-}
-__device__ __forceinline__ void read_row(float2 (&S)[HS / 2], const float *from)
-{
-#pragma unroll
-    for (int c = 0; c < HS / 2; c += 2) {
-        const float4 t = from ? load4(from + 2 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
-        S[c] = f2(t.x, t.y);
-        S[c + 1] = f2(t.z, t.w);
-    }
-}
-__device__ __forceinline__ void write_row(const float2 (&S)[HS / 2], float *to)
-{
-#pragma unroll
-    for (int c = 0; c < HS / 2; c += 2) store4(to + 2 * c, make_float4(S[c].x, S[c].y, S[c + 1].x, S[c + 1].y));
-}
-__device__ __forceinline__ void zero_half_row(unsigned char *tile, int row, int half)
-{
-#pragma unroll
-    for (int c = 0; c < 4; ++c) *piece(tile, row, 4 * half + c) = make_uint4(0u, 0u, 0u, 0u);
-}
-
 struct Work {
     int h, sl, tok0, len, chunks;
     const float *init;   // this head's columns of the state to start from, or null
@@ -539,12 +481,12 @@ ssm_chunk_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__
     wk.sl = blockIdx.x % slices;
     wk.h = blockIdx.x / slices % p.a.H;
     const int index = blockIdx.x / slices / p.a.H;
-    const Piece pc(p.a.cu_seqlens, p.a.T, p.parts, p.seg_len, index);
+    const Piece pc(p.a.cu_seqlens, p.a.T, p.parts, index);
     const size_t head = ((size_t)wk.h * N) * p.a.P + wk.sl * NS, state = (size_t)p.a.H * N * p.a.P;
     wk.tok0 = pc.tok0;
     wk.len = pc.len;
     wk.chunks = (pc.len + C - 1) / C;
-    wk.init = p.parts > 1 ? p.part_state + index * state + head : p.a.init_state ? p.a.init_state + pc.n * state + head : nullptr;
+    wk.init = p.parts.n > 1 ? p.parts.state + index * state + head : p.a.init_state ? p.a.init_state + pc.n * state + head : nullptr;
     wk.fin = p.a.final_state && pc.last ? p.a.final_state + pc.n * state + head : nullptr;
     if (pc.len <= 0) {   // an empty sequence hands its state on (its first part does)
         const size_t at = (size_t)(tid >> 1) * p.a.P + (tid & 1) * HS;
@@ -622,7 +564,7 @@ cudaError_t launch_t(const Params &p, cudaStream_t stream)
     constexpr int smem = (int)sizeof(Smem<std::is_same<OUT, float>::value ? 2 : 1>);
     const cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (err != cudaSuccess) return err;
-    kern<<<(unsigned)(p.a.n_seq * p.parts) * p.a.H * (p.a.P / NS), NT, smem, stream>>>(tq, tk, tv, p);
+    kern<<<(unsigned)(p.a.n_seq * p.parts.n) * p.a.H * (p.a.P / NS), NT, smem, stream>>>(tq, tk, tv, p);
     count_launch(1);
     return cudaGetLastError();
 }
@@ -645,9 +587,15 @@ bool make_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, 
 
 bool ssm_chunk_supported(int io_dtype, int N, int P, int rows) { return io_dtype == KLA_BF16 && (N == 64 || N == 128) && P % ssm::NS == 0 && rows > 0; }
 
+size_t ssm_chunk_workspace_bytes(const SsmParams &a) { return ssm::Parts(a, sm_count(), nullptr).bytes(a); }
+
 cudaError_t launch_ssm_chunk(const SsmParams &a, int out_dtype, cudaStream_t stream)
 {
-    ssm::Params p = {a, 1, a.cu_seqlens ? INT32_MAX / 2 : (a.T + ssm::C - 1) / ssm::C * ssm::C, nullptr, nullptr};
+    ssm::Params p = {a, ssm::Parts(a, sm_count(), a.workspace)};
+    if (p.parts.n > 1) {
+        const cudaError_t err = ssm::launch_part_starts(a, p.parts, false, stream);
+        if (err != cudaSuccess) return err;
+    }
     if (a.N == 64) return out_dtype == KLA_F32 ? ssm::launch_t<64, float>(p, stream) : ssm::launch_t<64, __nv_bfloat16>(p, stream);
     return out_dtype == KLA_F32 ? ssm::launch_t<128, float>(p, stream) : ssm::launch_t<128, __nv_bfloat16>(p, stream);
 }

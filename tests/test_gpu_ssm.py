@@ -11,7 +11,7 @@ import pytest
 import torch
 
 from layer_refs import check, grads, leaf, scan
-from paper_2605_08587_b200 import KLA_FLAG_FORCE_SIMT, KLA_FLAG_NONE, kla_ssm_bwd, kla_ssm_fwd, kla_ssm_step
+from paper_2605_08587_b200 import KLA_FLAG_FORCE_SIMT, KLA_FLAG_NO_SEGMENTS, KLA_FLAG_NONE, kla_ssm_bwd, kla_ssm_fwd, kla_ssm_step, launch_count
 
 DEV = "cuda:0"
 BF, F32 = torch.bfloat16, torch.float32
@@ -197,6 +197,25 @@ def test_gradient_against_differences(N, P):
         u /= u.norm()
         diff = (loss(dict(s, **{n: s[n] + h * u})) - loss(dict(s, **{n: s[n] - h * u}))) / (2 * h)
         assert abs(diff - float((g[d] * u).sum())) <= 4e-3 * max(1.0, float(g[d].norm())), n
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens, H, N, P", [([2000], 1, 128, 64), ([1500, 0, 7], 2, 64, 64), ([0, 1800, 129], 1, 128, 128), ([0, 0, 1300], 1, 64, 64)])
+@pytest.mark.parametrize("state", [False, True])
+def test_long_sequences_in_parts(lens, H, N, P, state):
+    """Cut into parts that run side by side, against the recurrence and against the uncut launch."""
+    s, seqs, dy, df = make(lens, H, 1, N, P, BF, state=state, seed=7)
+    y, f = kla_ssm_fwd(**s, **seqs, out_dtype=F32)
+    y1, f1 = kla_ssm_fwd(**s, **seqs, out_dtype=F32, flags=KLA_FLAG_NO_SEGMENTS)
+    n0 = launch_count()
+    kla_ssm_fwd(**s, **seqs)
+    assert launch_count() - n0 == 3      # what the parts add, their starts, the scan
+    _, (ry, rf), _, (my, mf) = reference(s, lens)
+    rel = rel_of(lens, N, P)
+    for got in (y, y1):
+        check(got[0], ry, my, rel, "out")
+    for got in (f, f1):
+        check(got, rf, mf, 2.0 ** -17 + (max(lens) + 64) * 2.0 ** -24, "final_state")
 
 
 @pytest.mark.gpu
