@@ -277,7 +277,8 @@ size_t kla_ssm_bwd_workspace_bytes(const kla_desc *desc, int32_t groups)
     int64_t rows = 0;
     if (check_rows(desc, &rows) != KLA_OK || check_sequences(desc) != KLA_OK) return 0;
     if (desc->H < 1 || groups < 1 || desc->H % groups || desc->d_k < 8 || desc->d_k > 256 || desc->d_v < 8 || desc->d_v > 256) return 0;
-    return ssm_bwd_workspace_bytes((int)rows, desc->n_seq, desc->H, groups, desc->d_k, desc->d_v);
+    const SsmParams p = ssm_sizes(desc, rows, groups);
+    return on_tensor_cores(desc, p) ? ssm_bwd_chunk_workspace_bytes(p) : ssm_bwd_workspace_bytes((int)rows, desc->n_seq, desc->H, groups, desc->d_k, desc->d_v);
 }
 
 kla_status kla_ssm_bwd(const kla_desc *desc, int32_t groups, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
@@ -301,6 +302,7 @@ kla_status kla_ssm_bwd(const kla_desc *desc, int32_t groups, const void *q, int6
     p.da = da;
     p.dd = dd;
     p.dinit = dinit_state;
+    if (on_tensor_cores(desc, p)) return launched(launch_ssm_bwd_chunk(p, (cudaStream_t)desc->stream));
     return launched(launch_ssm_bwd(p, desc->io_dtype, (cudaStream_t)desc->stream));
 }
 

@@ -89,5 +89,10 @@ size_t ssm_chunk_workspace_bytes(const SsmParams &p);
 cudaError_t launch_ssm_chunk(const SsmParams &p, int out_dtype, cudaStream_t stream);
 size_t ssm_bwd_workspace_bytes(int rows, int n_seq, int H, int G, int N, int P);
 cudaError_t launch_ssm_bwd(const SsmParams &p, int io_dtype, cudaStream_t stream);
+// da, dd [H] from partial sums [n][H], in their order (ssm_scan.cu).
+cudaError_t launch_ssm_sums(const float *part_a, const float *part_d, int n, int H, float *da, float *dd, cudaStream_t stream);
+// The reverse mode on the tensor cores (ssm_bwd.cu), where ssm_chunk_supported.
+size_t ssm_bwd_chunk_workspace_bytes(const SsmParams &p);
+cudaError_t launch_ssm_bwd_chunk(const SsmParams &p, cudaStream_t stream);
 
 }  // namespace kla

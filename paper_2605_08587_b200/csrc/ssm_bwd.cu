@@ -1,0 +1,639 @@
+// Reverse mode of the selective state space scan on the tensor cores (bf16; formulas at the top of ssm_scan.cu): chunks of 128 tokens.
+//
+// Two passes over the states (ssm_state.cu) leave, in fp32, the state S before every chunk and the gradient G of the state behind it; they are
+// independent of each other.  Then every (chunk, group of heads that share q and k) is by itself: a block takes one, and its heads one after another, each
+// in slices of 64 columns of v.  Per slice, with rows j and columns i of 128 x 128 products, do the gradient of o, parts as in ssm_chunk.cu:
+//
+//     DX^T = v do^T                           L_ij = exp(l_i - l_j);  (k q^T once per block)
+//     M_ji = L_ij dt_j (q_i . k_j)            dv  = M do + w_j (k G) + d do
+//     sum over heads of L_ij dt_j (do_i . v_j) in registers: one product each with q and k at the end gives their parts of dk and dq
+//     dq += (e^{l_i} do) S^T,  dk += (w_j v) G^T     w_j = dt_j e^{l_Q - l_j}; accumulated over the heads in tensor memory
+//     x_i = e^{l_i} (q S)_i . do_i,  z_j = w_j (k G)_j . v_j
+//
+// Precision.  dq, dk, dv are bf16: of their derived operands M, the sum over heads, the scaled do and v are one bf16 each, and S and G two, so that
+// every term carries one rounding like the result's own (with one part of S and G the 2-norm error of dq is 2.7e-3, the rounding alone 1.7e-3).
+// The gradients of dt and a are fp32: their terms come from exact products (DX, k q^T) and from S and G in three bf16 parts (24 bits), summed in fp32.
+//
+// 256 threads work, a thread to half a row; one warp issues the products and loads the tiles.  The chain of one slice is what takes the time, not the
+// products (about a third of it) nor memory.
+#include "ssm_pieces.cuh"
+
+namespace kla {
+namespace ssm {
+
+namespace {
+
+constexpr int NT = 256 + 128;   // (of the last warpgroup one warp works)
+
+enum Bar { B_QK = 0, B_CLEAN0, B_CB, B_TILES, B_CLEAN, B_DX, B_TOT, B_A, B_M, B_C1, B_B, B_C2, B_E, B_FREE, B_MS, B_FIN, B_COUNT };
+
+// Tensor memory: k q^T, dq, dk (128 columns each), DX^T (128); when that has been read, M do (64) and q S, then k G (64).
+constexpr uint32_t TM_CB = 0, TM_DQ = 128, TM_DK = 256, TM_DX = 384, TM_DV = 384, TM_SG = 448;
+
+struct Smem {
+    alignas(1024) unsigned char k[2][TILE], q[2][TILE];   // [64 of N][token][64]
+    alignas(1024) unsigned char v[TILE], go[TILE];        // [token][64 columns]
+    alignas(1024) unsigned char sp[3][TILE];              // parts of S, then of G: [row of N][64 columns]
+    alignas(1024) unsigned char m[2][TILE];               // M^T, at the end the sum over heads: [64 of i][j][64]
+    alignas(1024) unsigned char gs[TILE], vs[TILE];       // e^{l_i} do, w_j v
+    float a2[C], r[C];
+    float rows[4][C];         // sums over 32 tokens j of R_ij, j < i
+    float acc[2][4][C];       // of a token, by half of the columns: its own share of F (but for the sums of rows), z, what ddt has directly, do . v
+    float tot[2][4];
+    float sg[8];
+    alignas(8) uint64_t bar[B_COUNT];
+    uint32_t tmem;
+    volatile int abort_flag;
+};
+static_assert(sizeof(Smem) <= 232448, "shared memory of one block");
+
+struct Params {
+    SsmParams a;
+    const float *states, *dstates;    // [slot][H][P / 64][STATE_ELEMS]
+    float *part_a, *part_d;           // [slot][4][H]
+    float *part_q, *part_k;           // [splits][rows][G][N], or null: dq, dk are written
+    int splits;                       // blocks that share the heads of a group
+};
+
+// Lane l gets the sum over the warp of x[l].
+__device__ __forceinline__ float column_sums(float (&x)[32])
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int n = 16; n > 0; n >>= 1) {
+        const bool up = lane & n;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float keep = up ? x[i + n] : x[i], give = up ? x[i] : x[i + n];
+            x[i] = keep + __shfl_xor_sync(0xffffffffu, give, n);
+        }
+    }
+    return x[0];
+}
+
+__device__ __forceinline__ float dot_bf16(float2 a, uint32_t b, float s)
+{
+    const float2 y = unpack2(b);
+    return fmaf(a.x, y.x, fmaf(a.y, y.y, s));
+}
+
+template <int N>
+__device__ __forceinline__ void split_state(Smem &sm, const float2 (&S)[HS / 2])
+{
+    const int t = threadIdx.x & 127, half = threadIdx.x >> 7;
+    if (N == 64 && t >= N) return;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const uint32_t at = sw128(t, 4 * half + c);
+        float2 x[4] = {S[4 * c], S[4 * c + 1], S[4 * c + 2], S[4 * c + 3]};
+        *reinterpret_cast<uint4 *>(sm.sp[0] + at) = make_uint4(part(x[0]), part(x[1]), part(x[2]), part(x[3]));
+        *reinterpret_cast<uint4 *>(sm.sp[1] + at) = make_uint4(part(x[0]), part(x[1]), part(x[2]), part(x[3]));
+        *reinterpret_cast<uint4 *>(sm.sp[2] + at) = make_uint4(pack2(x[0]), pack2(x[1]), pack2(x[2]), pack2(x[3]));
+    }
+}
+__device__ __forceinline__ void load_state(float2 (&S)[HS / 2], const float *from)
+{
+#pragma unroll
+    for (int i = 0; i < HS / 4; ++i) {
+        const float4 t = load4(from + i * 1024);
+        S[2 * i] = f2(t.x, t.y);
+        S[2 * i + 1] = f2(t.z, t.w);
+    }
+}
+
+struct Work {
+    int slot, tok0, m, g, h0, items;   // first head, slices of all its heads
+};
+
+template <int N>
+__device__ void workers(Smem &sm, const Params &p, const Work &wk)
+{
+    const int t = threadIdx.x & 127, half = threadIdx.x >> 7, lane = t & 31, warp = t >> 5, slices = p.a.P / NS, m = wk.m;
+    const uint32_t tm = sm.tmem + ((uint32_t)(warp * 32) << 16);
+    const bool in = t < m, row = N == 128 || t < N;
+    auto wait = [&](int b, int parity) { return bar_wait(&sm.bar[b], parity, &sm.abort_flag); };
+    if (m < C) {   // rows behind the sequence's end are nobody's, or another sequence's
+        if (!wait(B_QK, 0)) return;
+        if (!in)
+#pragma unroll
+            for (int b = 0; b < N / 64; ++b) {
+                zero_half_row(sm.k[b], t, half);
+                zero_half_row(sm.q[b], t, half);
+            }
+        fence_async_smem();
+        mbar_arrive(&sm.bar[B_CLEAN0]);
+    }
+    float2 ms[32];   // sum over heads of L_ij dt_j (do_i . v_j): row j = t, columns i = 64 half ..
+#pragma unroll
+    for (int i = 0; i < 32; ++i) ms[i] = f2(0.f);
+    const size_t row_out = (size_t)(wk.tok0 + t);
+    auto state_at = [&](const float *base, int item) {
+        return base + (((size_t)wk.slot * p.a.H + wk.h0) * slices + item) * STATE_ELEMS + threadIdx.x * 4;
+    };
+    float2 S[HS / 2], G[HS / 2];
+    load_state(S, state_at(p.states, 0));
+    float dt = in ? p.a.dt[row_out * p.a.H + wk.h0] : 0.f;
+    // scalars of a head: this token's
+    float w = 0.f, wn = 0.f, e = 0.f, dt_now = 0.f, f0 = 0.f, f1 = 0.f, a2 = 0.f, a = 0.f, whole = 0.f;
+    float c_all = 0.f, c_diag = 0.f, z = 0.f, x = 0.f, dd = 0.f, sg = 0.f;   // sums over a head's slices
+    bool ok = wait(B_CB, 0);
+#pragma unroll 1
+    for (int it = 0; ok && it < wk.items; ++it) {
+        const int h = wk.h0 + it / slices, sl = it % slices;
+        // -- decays, once per head
+        if (sl == 0) {
+            a = p.a.a[h];
+            const BlockScan b(dt, a);
+            float *tot = sm.tot[h & 1];
+            if (lane == 0) {
+                if (half == 0) tot[warp] = b.tot;
+                mbar_arrive(&sm.bar[B_TOT]);
+            }
+            dt_now = dt;
+            a2 = b.a2;
+            const float r = exp2f(a2);
+            if (half == 0) sm.a2[t] = a2;
+            else sm.r[t] = r;
+            if (it + slices < wk.items) dt = in ? p.a.dt[row_out * p.a.H + h + 1] : 0.f;
+            if (!(ok = wait(B_TOT, it / slices))) break;
+            const float t0 = tot[0], t1 = tot[1], t2 = tot[2], t3 = tot[3];
+            e = r * exp2f(warp == 0 ? 0.f : warp == 1 ? t0 : warp == 2 ? t0 + t1 : t0 + t1 + t2);
+            wn = exp2f(b.rest + (warp == 0 ? t1 + t2 + t3 : warp == 1 ? t2 + t3 : warp == 2 ? t3 : 0.f));
+            w = dt_now * wn;
+            // from this token to the start of block 2 half, 2 half + 1 of the columns (where that lies behind this token's block)
+            f0 = exp2f(b.rest + (half == 0 ? 0.f : warp == 0 ? t1 : 0.f));
+            f1 = exp2f(b.rest + (half == 0 ? 0.f : warp == 0 ? t1 + t2 : warp == 1 ? t2 : 0.f));
+            whole = exp2f(t0 + t1 + t2 + t3);
+            c_all = c_diag = z = x = dd = sg = 0.f;
+        }
+        if (!(ok = wait(B_TILES, it))) break;
+        if (m < C) {
+            if (!in) {
+                zero_half_row(sm.v, t, half);
+                zero_half_row(sm.go, t, half);
+            }
+            fence_async_smem();
+            mbar_arrive(&sm.bar[B_CLEAN]);
+        }
+        // -- scaled tiles, parts of S
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t at = sw128(t, 4 * half + i);
+            const uint4 gv = *reinterpret_cast<const uint4 *>(sm.go + at), vv = *reinterpret_cast<const uint4 *>(sm.v + at);
+            const float2 e2 = f2(e), w2 = f2(w);
+            *reinterpret_cast<uint4 *>(sm.gs + at) = make_uint4(pack2(mul2(unpack2(gv.x), e2)), pack2(mul2(unpack2(gv.y), e2)), pack2(mul2(unpack2(gv.z), e2)), pack2(mul2(unpack2(gv.w), e2)));
+            *reinterpret_cast<uint4 *>(sm.vs + at) = make_uint4(pack2(mul2(unpack2(vv.x), w2)), pack2(mul2(unpack2(vv.y), w2)), pack2(mul2(unpack2(vv.z), w2)), pack2(mul2(unpack2(vv.w), w2)));
+            dd = dot_bf16(unpack2(gv.x), vv.x, dot_bf16(unpack2(gv.y), vv.y, dot_bf16(unpack2(gv.z), vv.z, dot_bf16(unpack2(gv.w), vv.w, dd))));
+        }
+        split_state<N>(sm, S);
+        fence_async_smem();
+        mbar_arrive(&sm.bar[B_A]);
+        load_state(G, state_at(p.dstates, it));
+        // -- M, the sum over heads, and the sums of R
+        if (!(ok = wait(B_A, it) && wait(B_DX, it))) break;   // (everybody's a2 and r, too)
+        tc_fence_after();
+#pragma unroll
+        for (int ii = 0; ii < 2; ++ii) {
+            const int I = 2 * half + ii;   // block of 32 columns i
+            float rs[32];
+#pragma unroll
+            for (int u = 0; u < 32; u += 16) {
+                float2 mm[8];
+                if (I < warp) {
+#pragma unroll
+                    for (int y = 0; y < 8; ++y) mm[y] = f2(0.f);
+                } else {
+                    float cb[16], dx[16];
+                    tmem_ld16(tm + TM_CB + I * 32 + u, cb);
+                    tmem_ld16(tm + TM_DX + I * 32 + u, dx);
+                    const float f = ii ? f1 : f0;
+#pragma unroll
+                    for (int y = 0; y < 16; y += 2) {
+                        const int i = I * 32 + u + y;
+                        float2 L;
+                        if (I > warp) {
+                            const float2 ri = *reinterpret_cast<const float2 *>(&sm.r[i]);
+                            L = mul2(ri, f2(f));
+                        } else {
+                            const float2 ai = *reinterpret_cast<const float2 *>(&sm.a2[i]);
+                            L.x = u + y >= lane ? ex2_approx(ai.x - a2) : 0.f;
+                            L.y = u + y + 1 >= lane ? ex2_approx(ai.y - a2) : 0.f;
+                        }
+                        const float2 d = f2(dx[y], dx[y + 1]), uu = mul2(L, f2(cb[y], cb[y + 1]));
+                        mm[y / 2] = mul2(uu, f2(dt_now));
+                        ms[ii * 16 + (u + y) / 2] = fma2(mul2(L, d), f2(dt_now), ms[ii * 16 + (u + y) / 2]);
+                        float2 rr = mul2(uu, d);
+                        c_all += rr.x + rr.y;
+                        if (I == warp) {
+                            if (u + y == lane) c_diag += rr.x, rr.x = 0.f;
+                            if (u + y + 1 == lane) c_diag += rr.y, rr.y = 0.f;
+                        }
+                        rs[u + y] = rr.x * dt_now;
+                        rs[u + y + 1] = rr.y * dt_now;
+                    }
+                }
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+                    *piece(sm.m[half], t, ii * 4 + (u >> 3) + y) = make_uint4(pack2(mm[4 * y]), pack2(mm[4 * y + 1]), pack2(mm[4 * y + 2]), pack2(mm[4 * y + 3]));
+            }
+            if (I >= warp) {
+                const float s = column_sums(rs);
+                sm.rows[warp][I * 32 + lane] = sl ? sm.rows[warp][I * 32 + lane] + s : s;
+            }
+        }
+        fence_async_smem();
+        tc_fence_before();
+        mbar_arrive(&sm.bar[B_M]);
+        // -- x, then the parts of G
+        if (!(ok = wait(B_C1, it))) break;
+        tc_fence_after();
+        {
+            float s = 0.f;
+#pragma unroll
+            for (int u = 0; u < 32; u += 16) {
+                float qs[16];
+                tmem_ld16(tm + TM_SG + half * 32 + u, qs);
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const uint4 gv = *piece(sm.go, t, 4 * half + (u >> 3) + y);
+                    s = dot_bf16(f2(qs[8 * y], qs[8 * y + 1]), gv.x, dot_bf16(f2(qs[8 * y + 2], qs[8 * y + 3]), gv.y, dot_bf16(f2(qs[8 * y + 4], qs[8 * y + 5]), gv.z, dot_bf16(f2(qs[8 * y + 6], qs[8 * y + 7]), gv.w, s))));
+                }
+            }
+            x = fmaf(e, s, x);
+        }
+        if (row)
+#pragma unroll
+            for (int i = 0; i < HS / 2; ++i) sg = fmaf(S[i].x, G[i].x, fmaf(S[i].y, G[i].y, sg));
+        split_state<N>(sm, G);
+        fence_async_smem();
+        tc_fence_before();
+        mbar_arrive(&sm.bar[B_B]);
+        if (it + 1 < wk.items) load_state(S, state_at(p.states, it + 1));
+        // -- dv and z
+        if (!(ok = wait(B_C2, it))) break;
+        tc_fence_after();
+        {
+            const float2 skip = f2(p.a.skip ? p.a.skip[h] : 0.f), w2 = f2(w);
+            float s = 0.f;
+#pragma unroll
+            for (int u = 0; u < 32; u += 16) {
+                float kg[16], dv[16];
+                tmem_ld16(tm + TM_SG + half * 32 + u, kg);
+                tmem_ld16(tm + TM_DV + half * 32 + u, dv);
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const uint4 vv = *piece(sm.v, t, 4 * half + (u >> 3) + y), gv = *piece(sm.go, t, 4 * half + (u >> 3) + y);
+                    const uint32_t vw[4] = {vv.x, vv.y, vv.z, vv.w}, gw[4] = {gv.x, gv.y, gv.z, gv.w};
+                    uint32_t o[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float2 kk = f2(kg[8 * y + 2 * q], kg[8 * y + 2 * q + 1]);
+                        s = dot_bf16(kk, vw[q], s);
+                        o[q] = pack2(fma2(skip, unpack2(gw[q]), fma2(w2, kk, f2(dv[8 * y + 2 * q], dv[8 * y + 2 * q + 1]))));
+                    }
+                    *piece(sm.gs, t, 4 * half + (u >> 3) + y) = make_uint4(o[0], o[1], o[2], o[3]);   // (read by the products that have completed)
+                }
+            }
+            z += s;   // (without w_j)
+        }
+        tc_fence_before();
+        __syncwarp();
+        {
+            __nv_bfloat16 *dv = static_cast<__nv_bfloat16 *>(p.a.dv) + ((size_t)wk.tok0 * p.a.H + h) * p.a.P + sl * NS + half * 32 + (lane & 3) * 8;
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+                const int rr = warp * 32 + i + (lane >> 2);
+                if (rr < m) *reinterpret_cast<uint4 *>(dv + (size_t)rr * p.a.H * p.a.P) = *piece(sm.gs, rr, 4 * half + (lane & 3));
+            }
+        }
+        __syncwarp();
+        mbar_arrive(&sm.bar[B_FREE]);
+        // -- gradients of dt and a, behind a head's last slice
+        if (sl == slices - 1) {
+            sm.acc[half][0][t] = x - dt_now * (c_all - c_diag);
+            sm.acc[half][1][t] = w * z;
+            sm.acc[half][2][t] = fmaf(wn, z, c_all);
+            sm.acc[half][3][t] = dd;
+            for (int o = 16; o > 0; o >>= 1) sg += __shfl_xor_sync(0xffffffffu, sg, o);
+            if (lane == 0) sm.sg[threadIdx.x >> 5] = sg;
+            mbar_arrive(&sm.bar[B_E]);
+            if (!(ok = wait(B_E, it / slices))) break;
+            if (half == 0) {   // a warp to 32 tokens; of the others' it needs the sums
+                float all = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) all += sm.sg[i];
+                float later = 0.f, earlier = 0.f, own = 0.f, zt = 0.f;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int i = b * 32 + lane;
+                    float o = 0.f, y = 0.f;
+                    if (b >= warp) {
+                        o = sm.acc[0][0][i] + sm.acc[1][0][i];
+#pragma unroll
+                        for (int J = 0; J <= b; ++J) o += sm.rows[J][i];
+                    }
+                    if (b <= warp) y = sm.acc[0][1][i] + sm.acc[1][1][i];
+                    if (b > warp) later += o;
+                    if (b == warp) own = o, zt = y;
+                    if (b < warp) earlier += y;
+                }
+                float suffix = own, prefix = zt;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const float u = __shfl_down_sync(0xffffffffu, suffix, o), y = __shfl_up_sync(0xffffffffu, prefix, o);
+                    if (lane + o < 32) suffix += u;
+                    if (lane >= o) prefix += y;
+                    later += __shfl_xor_sync(0xffffffffu, later, o);
+                    earlier += __shfl_xor_sync(0xffffffffu, earlier, o);
+                }
+                const float before = __shfl_up_sync(0xffffffffu, prefix, 1);
+                const float F = suffix + later + (lane ? before : 0.f) + earlier + whole * all;
+                if (in) p.a.ddt[row_out * p.a.H + h] = fmaf(a, F, sm.acc[0][2][t] + sm.acc[1][2][t]);
+                float da = in ? dt_now * F : 0.f, d = sm.acc[0][3][t] + sm.acc[1][3][t];
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) {
+                    da += __shfl_xor_sync(0xffffffffu, da, o);
+                    d += __shfl_xor_sync(0xffffffffu, d, o);
+                }
+                if (lane == 0) {
+                    p.part_a[((size_t)wk.slot * 4 + warp) * p.a.H + h] = da;
+                    p.part_d[((size_t)wk.slot * 4 + warp) * p.a.H + h] = d;
+                }
+            }
+        }
+    }
+    if (!ok || sm.abort_flag) return;
+    // -- the heads' sum as an operand, row j
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        *piece(sm.m[half], t, i) = make_uint4(pack2(ms[4 * i]), pack2(ms[4 * i + 1]), pack2(ms[4 * i + 2]), pack2(ms[4 * i + 3]));
+    fence_async_smem();
+    tc_fence_before();
+    mbar_arrive(&sm.bar[B_MS]);
+    if (!wait(B_FIN, 0)) return;
+    tc_fence_after();
+    constexpr int W = N / 2;   // columns of a thread
+    const size_t at = (row_out * p.a.G + wk.g) * N + half * W;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float *part = which ? p.part_k : p.part_q;
+        __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(which ? p.a.dk : p.a.dq) + at;
+        if (part) part += (size_t)(blockIdx.x % p.splits) * p.a.rows * p.a.G * N + at;
+#pragma unroll
+        for (int c = 0; c < W; c += 16) {
+            float v[16];
+            tmem_ld16(tm + (which ? TM_DK : TM_DQ) + half * W + c, v);
+            if (!in) continue;
+            if (part) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) store4(part + c + i, make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; i += 8)
+                    *reinterpret_cast<uint4 *>(out + c + i) = make_uint4(pack2(f2(v[i], v[i + 1])), pack2(f2(v[i + 2], v[i + 3])), pack2(f2(v[i + 4], v[i + 5])), pack2(f2(v[i + 6], v[i + 7])));
+            }
+        }
+    }
+    tc_fence_before();
+}
+
+// One warp: products and tiles.
+template <int N>
+__device__ void issue(Smem &sm, const CUtensorMap *tq, const CUtensorMap *tk, const CUtensorMap *tv, const CUtensorMap *tg, const Params &p, const Work &wk)
+{
+    constexpr int NB = N / 64;
+    constexpr uint32_t T16 = TILE / 16;
+    const bool first = (threadIdx.x & 31) == 0;
+    const int slices = p.a.P / NS, xk = wk.g * N;
+    const uint32_t tm = sm.tmem;
+    auto wait = [&](int b, int parity) {
+        const bool ok = bar_wait(&sm.bar[b], parity, &sm.abort_flag);
+        tc_fence_after();
+        return ok;
+    };
+    auto desc = [](const void *x, uint32_t lbo) { return desc_lo(smem_desc_sw128(smem_u32(x), lbo, 1024)); };
+    if (first) {
+        mbar_expect_tx(&sm.bar[B_QK], 2 * NB * TILE);
+        for (int b = 0; b < NB; ++b) {
+            tma_load_2d(sm.k[b], tk, xk + b * 64, wk.tok0, &sm.bar[B_QK]);
+            tma_load_2d(sm.q[b], tq, xk + b * 64, wk.tok0, &sm.bar[B_QK]);
+        }
+    }
+    __syncwarp();
+    auto load = [&](int it) {
+        if (first) {
+            const int x = (wk.h0 + it / slices) * p.a.P + it % slices * NS;
+            mbar_expect_tx(&sm.bar[B_TILES], 2 * TILE);
+            tma_load_2d(sm.v, tv, x, wk.tok0, &sm.bar[B_TILES]);
+            tma_load_2d(sm.go, tg, x, wk.tok0, &sm.bar[B_TILES]);
+            if (it + 1 < wk.items) {
+                const int y = (wk.h0 + (it + 1) / slices) * p.a.P + (it + 1) % slices * NS;
+                prefetch_2d(tv, y, wk.tok0);
+                prefetch_2d(tg, y, wk.tok0);
+            }
+        }
+        __syncwarp();
+    };
+    load(0);
+    if (!wait(B_QK, 0) || (wk.m < C && !wait(B_CLEAN0, 0))) return;
+    const uint32_t k_km = desc(sm.k, 0), q_km = desc(sm.q, 0), v_km = desc(sm.v, 0), go_km = desc(sm.go, 0), gs_km = desc(sm.gs, 0), vs_km = desc(sm.vs, 0);
+    const uint32_t sp_km = desc(sm.sp, 0), m_km = desc(sm.m, 0), m_mn = desc(sm.m, TILE), k_mn = desc(sm.k, TILE), q_mn = desc(sm.q, TILE);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) mma4_bf16_lo<2, 2>(tm + TM_CB, k_km + b * T16, q_km + b * T16, idesc_bf16(128, 128, 0, 0), b > 0);
+    mma_commit(&sm.bar[B_CB]);
+#pragma unroll 1
+    for (int it = 0; it < wk.items; ++it) {
+        if (it > 0) {
+            if (!wait(B_FREE, it - 1)) return;
+            load(it);
+        }
+        if (!wait(B_TILES, it) || (wk.m < C && !wait(B_CLEAN, it))) return;
+        mma4_bf16_lo<2, 2>(tm + TM_DX, v_km, go_km, idesc_bf16(128, 128, 0, 0), 0);
+        mma_commit(&sm.bar[B_DX]);
+        if (!wait(B_A, it)) return;
+        mma4_bf16_lo<2, 2>(tm + TM_DQ, gs_km, sp_km + T16, idesc_bf16(128, N, 0, 0), it > 0);
+        mma4_bf16_lo<2, 2>(tm + TM_DQ, gs_km, sp_km, idesc_bf16(128, N, 0, 0), 1);
+        if (!wait(B_M, it)) return;
+#pragma unroll 1
+        for (int part = 2; part >= 0; --part)   // smallest first
+#pragma unroll
+            for (int b = 0; b < NB; ++b) mma4_bf16_lo<2, 128>(tm + TM_SG, q_km + b * T16, sp_km + part * T16 + b * 512, idesc_bf16(128, 64, 0, 1), part < 2 || b > 0);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) mma4_bf16_lo<2, 128>(tm + TM_DV, m_km + b * T16, go_km + b * 512, idesc_bf16(128, 64, 0, 1), b);
+        mma_commit(&sm.bar[B_C1]);
+        if (!wait(B_B, it)) return;
+#pragma unroll 1
+        for (int part = 2; part >= 0; --part)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) mma4_bf16_lo<2, 128>(tm + TM_SG, k_km + b * T16, sp_km + part * T16 + b * 512, idesc_bf16(128, 64, 0, 1), part < 2 || b > 0);
+        mma4_bf16_lo<2, 2>(tm + TM_DK, vs_km, sp_km + T16, idesc_bf16(128, N, 0, 0), it > 0);
+        mma4_bf16_lo<2, 2>(tm + TM_DK, vs_km, sp_km, idesc_bf16(128, N, 0, 0), 1);
+        if (p.a.test_timeout) return;   // test hook: the workers' wait for these products runs out
+        mma_commit(&sm.bar[B_C2]);
+    }
+    if (!wait(B_MS, 0)) return;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) mma4_bf16_lo<2, 128>(tm + TM_DK, m_km + b * T16, q_mn + b * 512, idesc_bf16(128, N, 0, 1), 1);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) mma4_bf16_lo<128, 128>(tm + TM_DQ, m_mn + b * 512, k_mn + b * 512, idesc_bf16(128, N, 1, 1), 1);
+    mma_commit(&sm.bar[B_FIN]);
+}
+
+template <int N>
+__global__ void __launch_bounds__(NT, 1)
+ssm_grads_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
+                    const __grid_constant__ CUtensorMap tg, const __grid_constant__ Params p)
+{
+    extern __shared__ __align__(1024) unsigned char smem_dyn[];
+    Smem &sm = *reinterpret_cast<Smem *>(smem_dyn);
+    if (smem_u32(smem_dyn) & 1023) {
+        if (threadIdx.x == 0 && p.a.status_word) atomicExch(p.a.status_word, (int)KLA_ERR_ALIGN);
+        return;
+    }
+    const int tid = threadIdx.x, per = p.a.H / p.a.G, each = (per + p.splits - 1) / p.splits, split = blockIdx.x % p.splits;
+    Work wk;
+    wk.g = blockIdx.x / p.splits % p.a.G;
+    wk.slot = blockIdx.x / p.splits / p.a.G;
+    wk.h0 = wk.g * per + split * each;
+    wk.items = min(each, per - split * each) * (p.a.P / NS);
+    const Slots slots(p.a.cu_seqlens, p.a.T);
+    int n = 0, hi = p.a.n_seq;   // the sequence whose first slot is the last one at or before this
+    while (hi - n > 1) {
+        const int mid = (n + hi) >> 1;
+        if (slots.first(mid) <= (size_t)wk.slot) n = mid;
+        else hi = mid;
+    }
+    const int start = p.a.cu_seqlens ? p.a.cu_seqlens[n] : n * p.a.T, end = p.a.cu_seqlens ? p.a.cu_seqlens[n + 1] : start + p.a.T;
+    wk.tok0 = start + (wk.slot - (int)slots.first(n)) * C;
+    wk.m = min(C, end - wk.tok0);
+    if (wk.m <= 0) {   // a slot that no chunk has
+        for (int i = tid; i < 4 * (wk.items / (p.a.P / NS)); i += NT) {
+            const size_t at = ((size_t)wk.slot * 4 + (i & 3)) * p.a.H + wk.h0 + (i >> 2);
+            p.part_a[at] = p.part_d[at] = 0.f;
+        }
+        return;
+    }
+    if (tid == 0) {
+        for (int b = 0; b < B_COUNT; ++b)
+            mbar_init(&sm.bar[b], b == B_TOT ? 8 : b == B_CLEAN0 || b == B_CLEAN || b == B_A || b == B_M || b == B_B || b == B_E || b == B_FREE || b == B_MS ? 256 : 1);
+        sm.abort_flag = 0;
+        mbar_fence_init();
+        tma_prefetch_desc(&tq);
+        tma_prefetch_desc(&tk);
+        tma_prefetch_desc(&tv);
+        tma_prefetch_desc(&tg);
+    }
+    if (tid >= 256 && tid < 288) tmem_alloc(&sm.tmem, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    // 384 threads x 168 registers at launch = 128 x (2 x 232 + 40)
+    if (tid < 256) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        workers<N>(sm, p, wk);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (tid < 288) issue<N>(sm, &tq, &tk, &tv, &tg, p, wk);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (sm.abort_flag) {   // copies and products issued just before a wait gave up finish first
+        for (int i = 0; i < 32; ++i) __nanosleep(1000);
+        if (tid == 0 && p.a.status_word) atomicExch(p.a.status_word, (int)KLA_ERR_TIMEOUT);
+    }
+    if (tid >= 256 && tid < 288) {
+        tc_fence_after();
+        tmem_dealloc(sm.tmem, 512);
+    }
+}
+
+// dq, dk from the partial sums of the blocks that shared a group's heads, in their order
+__global__ void __launch_bounds__(256) ssm_join_splits_kernel(const float *part_q, const float *part_k, int splits, size_t n, __nv_bfloat16 *dq, __nv_bfloat16 *dk)
+{
+    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    const float *part = blockIdx.y ? part_k : part_q;
+    float4 s = load4(part + i);
+    for (int k = 1; k < splits; ++k) {
+        const float4 t = load4(part + (size_t)k * n + i);
+        s = make_float4(s.x + t.x, s.y + t.y, s.z + t.z, s.w + t.w);
+    }
+    store4((blockIdx.y ? dk : dq) + i, s);
+}
+
+// Blocks that share a group's heads: as many as it takes to give every SM one.
+int splits_of(const SsmParams &a)
+{
+    const long long blocks = ((long long)a.rows / C + a.n_seq) * a.G;
+    const int per = a.H / a.G, want = (int)(sm_count() / blocks);
+    if (want <= 1 || per == 1) return 1;
+    const int each = (per + want - 1) / want;
+    return (per + each - 1) / each;
+}
+struct Layout {   // of the workspace, in bytes
+    size_t states, dstates, part_a, part_d, part_q, part_k, parts, all;
+    int splits;
+    explicit Layout(const SsmParams &a)
+    {
+        const size_t slots = (size_t)a.rows / C + a.n_seq, unit = slots * a.H * (a.P / NS) * STATE_ELEMS * sizeof(float);
+        auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+        splits = splits_of(a);
+        const size_t sums = up(slots * 4 * a.H * sizeof(float)), qk = splits > 1 ? up((size_t)splits * a.rows * a.G * a.N * sizeof(float)) : 0;
+        states = 0;
+        dstates = unit;
+        part_a = dstates + unit;
+        part_d = part_a + sums;
+        part_q = part_d + sums;
+        part_k = part_q + qk;
+        parts = part_k + qk;
+        all = parts + Parts(a, sm_count(), nullptr).bytes(a);
+    }
+};
+
+template <int N>
+cudaError_t launch_t(const Params &p, cudaStream_t stream)
+{
+    CUtensorMap tq, tk, tv, tg;
+    const uint64_t rows = (uint64_t)p.a.rows, kw = (uint64_t)p.a.G * N, vw = (uint64_t)p.a.H * p.a.P;
+    if (!make_map(&tq, p.a.q, rows, kw, p.a.q_stride) || !make_map(&tk, p.a.k, rows, kw, p.a.k_stride) || !make_map(&tv, p.a.v, rows, vw, p.a.v_stride) ||
+        !make_map(&tg, p.a.d_out, rows, vw, vw))
+        return cudaErrorInvalidValue;
+    auto kern = ssm_grads_tc_kernel<N>;
+    const cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
+    if (err != cudaSuccess) return err;
+    kern<<<(unsigned)((p.a.rows / C + p.a.n_seq) * p.a.G * p.splits), NT, sizeof(Smem), stream>>>(tq, tk, tv, tg, p);
+    count_launch(1);
+    return cudaGetLastError();
+}
+
+}  // namespace
+}  // namespace ssm
+
+size_t ssm_bwd_chunk_workspace_bytes(const SsmParams &a) { return ssm::Layout(a).all; }
+
+cudaError_t launch_ssm_bwd_chunk(const SsmParams &a, cudaStream_t stream)
+{
+    using namespace ssm;
+    const Layout l(a);
+    char *ws = static_cast<char *>(a.workspace);
+    auto at = [&](size_t x) { return reinterpret_cast<float *>(ws + x); };
+    const Parts parts(a, sm_count(), ws + l.parts);
+    for (int reverse = 0; reverse < 2; ++reverse) {
+        cudaError_t err = cudaSuccess;
+        if (parts.n > 1) err = launch_part_starts(a, parts, reverse, stream);
+        if (err == cudaSuccess) err = launch_chunk_states(a, parts, reverse, at(reverse ? l.dstates : l.states), stream);
+        if (err != cudaSuccess) return err;
+    }
+    const bool split = l.splits > 1;
+    const Params p = {a, at(l.states), at(l.dstates), at(l.part_a), at(l.part_d), split ? at(l.part_q) : nullptr, split ? at(l.part_k) : nullptr, l.splits};
+    cudaError_t err = a.N == 64 ? launch_t<64>(p, stream) : launch_t<128>(p, stream);
+    if (err != cudaSuccess) return err;
+    if (split) {
+        const size_t n = (size_t)a.rows * a.G * a.N;
+        ssm_join_splits_kernel<<<dim3((unsigned)((n / 4 + 255) / 256), 2), 256, 0, stream>>>(p.part_q, p.part_k, l.splits, n, static_cast<__nv_bfloat16 *>(a.dq), static_cast<__nv_bfloat16 *>(a.dk));
+        count_launch(1);
+    }
+    return launch_ssm_sums(p.part_a, p.part_d, (int)((a.rows / C + a.n_seq) * 4), a.H, a.da, a.dd, stream);
+}
+
+}  // namespace kla

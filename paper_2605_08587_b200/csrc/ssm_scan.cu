@@ -3,7 +3,7 @@
 //     S_t = exp(dt_t a) S_{t-1} + dt_t k_t v_t^T,     o_t = S_t^T q_t + d v_t,
 //
 // q and k shared by the H / G heads of a group.  This file: the recurrence in fp32 on CUDA cores for any N and P (multiples of 8 up to
-// 256), one token of it, and the reverse mode by chunks.  bf16 calls with N of 64 or 128 and P a multiple of 64 go to ssm_chunk.cu.
+// 256), one token of it, and the reverse mode by chunks.  bf16 calls with N of 64 or 128 and P a multiple of 64 go to ssm_chunk.cu and ssm_bwd.cu.
 //
 // Reverse mode of one chunk of tokens (l_i: sum of dt a up to and with token i, l_Q of the whole chunk; S: the state before the
 // chunk; G: the gradient of the state behind it; L_ij = exp(l_i - l_j) for j <= i):
@@ -500,6 +500,13 @@ size_t ssm_bwd_workspace_bytes(int rows, int n_seq, int H, int G, int N, int P)
     return slots * H * ((size_t)2 * N * P + 2) * sizeof(float);
 }
 
+cudaError_t launch_ssm_sums(const float *part_a, const float *part_d, int n, int H, float *da, float *dd, cudaStream_t stream)
+{
+    ssm_reduce_kernel<<<dim3((unsigned)ceil_div(H, 32), 2), 512, 0, stream>>>(part_a, part_d, n, H, da, dd);
+    count_launch(1);
+    return cudaGetLastError();
+}
+
 template <typename IO>
 static cudaError_t ssm_bwd_t(const SsmParams &p, cudaStream_t stream)
 {
@@ -518,9 +525,8 @@ static cudaError_t ssm_bwd_t(const SsmParams &p, cudaStream_t stream)
     err = cudaFuncSetAttribute(ssm_grads_kernel<IO>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (err != cudaSuccess) return err;
     ssm_grads_kernel<IO><<<(unsigned)(slots * p.G), 256, smem, stream>>>(p, seqs, states, dstates, part_a, part_d);
-    ssm_reduce_kernel<<<dim3((unsigned)ceil_div(p.H, 32), 2), 512, 0, stream>>>(part_a, part_d, (int)slots, p.H, p.da, p.dd);
-    count_launch(2);
-    return cudaGetLastError();
+    count_launch(1);
+    return launch_ssm_sums(part_a, part_d, (int)slots, p.H, p.da, p.dd, stream);
 }
 cudaError_t launch_ssm_bwd(const SsmParams &p, int io_dtype, cudaStream_t stream)
 {
