@@ -25,9 +25,20 @@ namespace {
 
 constexpr int NT = 256 + 128;   // (of the last warpgroup one warp works)
 
-enum Bar { B_QK = 0, B_CLEAN0, B_CB, B_TILES, B_CLEAN, B_DX, B_TOT, B_A, B_M, B_C1, B_B, B_C2, B_E, B_FREE, B_MS, B_FIN, B_COUNT };
+enum Bar {
+    B_QK = 0,       // q and k landed
+    B_TILES,        // v and do landed
+    B_CB, B_QS, B_DQ, B_DX, B_C2, B_FIN,   // products complete: k q^T; q S; its share of dq; DX^T; M do, k G and dk's share; the last ones
+    B_TOT,          // sums over 32 tokens written (a warp)
+    B_CLEAN0, B_CLEAN,   // rows behind the sequence's end zeroed: of q and k, of v and do (all workers, like those below)
+    B_S, B_SCALED, B_X, B_G, B_M,   // written: parts of S; scaled tiles; x read; parts of G; M
+    B_E,            // a head's sums written
+    B_FREE,         // a slice's tiles and accumulators read
+    B_MS,           // the sum over heads written
+    B_COUNT
+};
 
-// Tensor memory: k q^T, dq, dk (128 columns each), DX^T (128); when that has been read, M do (64) and q S, then k G (64).
+// Tensor memory: k q^T, dq, dk (128 columns each); q S (64), then DX^T (128), then M do (64) and k G (64).
 constexpr uint32_t TM_CB = 0, TM_DQ = 128, TM_DK = 256, TM_DX = 384, TM_DV = 384, TM_SG = 448;
 
 struct Smem {
@@ -36,7 +47,7 @@ struct Smem {
     alignas(1024) unsigned char sp[3][TILE];              // parts of S, then of G: [row of N][64 columns]
     alignas(1024) unsigned char m[2][TILE];               // M^T, at the end the sum over heads: [64 of i][j][64]
     alignas(1024) unsigned char gs[TILE], vs[TILE];       // e^{l_i} do, w_j v
-    float a2[C], r[C];
+    float a2[2][C], r[2][C];  // of heads in turn
     float rows[4][C];         // sums over 32 tokens j of R_ij, j < i
     float acc[2][4][C];       // of a token, by half of the columns: its own share of F (but for the sums of rows), z, what ddt has directly, do . v
     float tot[2][4];
@@ -105,6 +116,31 @@ struct Work {
     int slot, tok0, m, g, h0, items;   // first head, slices of all its heads
 };
 
+// 16 columns of two accumulators
+__device__ __forceinline__ void tmem_ld16x2(uint32_t ta, uint32_t tb, float (&a)[16], float (&b)[16])
+{
+    uint32_t x[16], y[16];
+#define R16(r) "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), \
+               "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : R16(x), R16(y) : "r"(ta), "r"(tb) : "memory");
+#undef R16
+#pragma unroll
+    for (int i = 0; i < 16; ++i) a[i] = __uint_as_float(x[i]), b[i] = __uint_as_float(y[i]);
+}
+
+// A head's scalars of one token.
+struct Head {
+    float dt, a, a2;
+    float w, wn;      // dt_j e^{l_Q - l_j}, and without dt_j
+    float e;          // e^{l_i}
+    float f0, f1;     // decay from this token to the start of block 2 half, 2 half + 1 of the columns (where that lies behind this token's block)
+    float whole;      // e^{l_Q}
+};
+
 template <int N>
 __device__ void workers(Smem &sm, const Params &p, const Work &wk)
 {
@@ -132,40 +168,91 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
     };
     float2 S[HS / 2], G[HS / 2];
     load_state(S, state_at(p.states, 0));
-    float dt = in ? p.a.dt[row_out * p.a.H + wk.h0] : 0.f;
-    // scalars of a head: this token's
-    float w = 0.f, wn = 0.f, e = 0.f, dt_now = 0.f, f0 = 0.f, f1 = 0.f, a2 = 0.f, a = 0.f, whole = 0.f;
+    const int heads = wk.items / slices;
+    float next_dt = in ? p.a.dt[row_out * p.a.H + wk.h0] : 0.f;
+    auto decays = [&](int i, Head &hd) {   // of the i-th head
+        const int h = wk.h0 + i;
+        hd.a = p.a.a[h];
+        hd.dt = next_dt;
+        const BlockScan b(hd.dt, hd.a);
+        float *tot = sm.tot[i & 1];
+        if (lane == 0) {
+            if (half == 0) tot[warp] = b.tot;
+            mbar_arrive(&sm.bar[B_TOT]);
+        }
+        hd.a2 = b.a2;
+        const float r = exp2f(b.a2);
+        if (half == 0) sm.a2[i & 1][t] = b.a2;
+        else sm.r[i & 1][t] = r;
+        if (i + 1 < heads) next_dt = in ? p.a.dt[row_out * p.a.H + h + 1] : 0.f;
+        if (!wait(B_TOT, i)) return false;
+        const float t0 = tot[0], t1 = tot[1], t2 = tot[2], t3 = tot[3];
+        hd.e = r * exp2f(warp == 0 ? 0.f : warp == 1 ? t0 : warp == 2 ? t0 + t1 : t0 + t1 + t2);
+        hd.wn = exp2f(b.rest + (warp == 0 ? t1 + t2 + t3 : warp == 1 ? t2 + t3 : warp == 2 ? t3 : 0.f));
+        hd.w = hd.dt * hd.wn;
+        hd.f0 = exp2f(b.rest + (half == 0 ? 0.f : warp == 0 ? t1 : 0.f));
+        hd.f1 = exp2f(b.rest + (half == 0 ? 0.f : warp == 0 ? t1 + t2 : warp == 1 ? t2 : 0.f));
+        hd.whole = exp2f(t0 + t1 + t2 + t3);
+        return true;
+    };
+    // Gradients of dt and a of the i-th head, a thread of the first half to a token; of the other blocks' tokens it needs the sums.
+    auto finish = [&](int i, float a, float dt, float whole) {
+        if (!wait(B_E, i)) return false;
+        if (half) return true;
+        const int h = wk.h0 + i;
+        float all = 0.f, later = 0.f, earlier = 0.f, own = 0.f, zt = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) all += sm.sg[k];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int at = b * 32 + lane;
+            float o = 0.f, y = 0.f;
+            if (b >= warp) {
+                o = sm.acc[0][0][at] + sm.acc[1][0][at];
+#pragma unroll
+                for (int J = 0; J <= b; ++J) o += sm.rows[J][at];
+            }
+            if (b <= warp) y = sm.acc[0][1][at] + sm.acc[1][1][at];
+            if (b > warp) later += o;
+            if (b == warp) own = o, zt = y;
+            if (b < warp) earlier += y;
+        }
+        float suffix = own, prefix = zt, d = sm.acc[0][3][t] + sm.acc[1][3][t];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const float u = __shfl_down_sync(0xffffffffu, suffix, o), y = __shfl_up_sync(0xffffffffu, prefix, o);
+            if (lane + o < 32) suffix += u;
+            if (lane >= o) prefix += y;
+            later += __shfl_xor_sync(0xffffffffu, later, o);
+            earlier += __shfl_xor_sync(0xffffffffu, earlier, o);
+        }
+        const float before = __shfl_up_sync(0xffffffffu, prefix, 1);
+        const float F = suffix + later + (lane ? before : 0.f) + earlier + whole * all;
+        if (in) p.a.ddt[row_out * p.a.H + h] = fmaf(a, F, sm.acc[0][2][t] + sm.acc[1][2][t]);
+        float da = in ? dt * F : 0.f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            da += __shfl_xor_sync(0xffffffffu, da, o);
+            d += __shfl_xor_sync(0xffffffffu, d, o);
+        }
+        if (lane == 0) {
+            p.part_a[((size_t)wk.slot * 4 + warp) * p.a.H + h] = da;
+            p.part_d[((size_t)wk.slot * 4 + warp) * p.a.H + h] = d;
+        }
+        return true;
+    };
+    Head hd, next;
     float c_all = 0.f, c_diag = 0.f, z = 0.f, x = 0.f, dd = 0.f, sg = 0.f;   // sums over a head's slices
-    bool ok = wait(B_CB, 0);
+    float old_a = 0.f, old_dt = 0.f, old_whole = 0.f;                        // of the head before
+    bool ok = decays(0, hd) && wait(B_CB, 0);
 #pragma unroll 1
     for (int it = 0; ok && it < wk.items; ++it) {
-        const int h = wk.h0 + it / slices, sl = it % slices;
-        // -- decays, once per head
-        if (sl == 0) {
-            a = p.a.a[h];
-            const BlockScan b(dt, a);
-            float *tot = sm.tot[h & 1];
-            if (lane == 0) {
-                if (half == 0) tot[warp] = b.tot;
-                mbar_arrive(&sm.bar[B_TOT]);
-            }
-            dt_now = dt;
-            a2 = b.a2;
-            const float r = exp2f(a2);
-            if (half == 0) sm.a2[t] = a2;
-            else sm.r[t] = r;
-            if (it + slices < wk.items) dt = in ? p.a.dt[row_out * p.a.H + h + 1] : 0.f;
-            if (!(ok = wait(B_TOT, it / slices))) break;
-            const float t0 = tot[0], t1 = tot[1], t2 = tot[2], t3 = tot[3];
-            e = r * exp2f(warp == 0 ? 0.f : warp == 1 ? t0 : warp == 2 ? t0 + t1 : t0 + t1 + t2);
-            wn = exp2f(b.rest + (warp == 0 ? t1 + t2 + t3 : warp == 1 ? t2 + t3 : warp == 2 ? t3 : 0.f));
-            w = dt_now * wn;
-            // from this token to the start of block 2 half, 2 half + 1 of the columns (where that lies behind this token's block)
-            f0 = exp2f(b.rest + (half == 0 ? 0.f : warp == 0 ? t1 : 0.f));
-            f1 = exp2f(b.rest + (half == 0 ? 0.f : warp == 0 ? t1 + t2 : warp == 1 ? t2 : 0.f));
-            whole = exp2f(t0 + t1 + t2 + t3);
-            c_all = c_diag = z = x = dd = sg = 0.f;
-        }
+        const int i = it / slices, h = wk.h0 + i, sl = it % slices;
+        // -- parts of S
+        split_state<N>(sm, S);
+        fence_async_smem();
+        mbar_arrive(&sm.bar[B_S]);
+        // -- scaled tiles, while q S is formed
         if (!(ok = wait(B_TILES, it))) break;
         if (m < C) {
             if (!in) {
@@ -175,23 +262,48 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
             fence_async_smem();
             mbar_arrive(&sm.bar[B_CLEAN]);
         }
-        // -- scaled tiles, parts of S
-#pragma unroll 1
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t at = sw128(t, 4 * half + i);
+#pragma unroll 2
+        for (int c = 0; c < 4; ++c) {
+            const uint32_t at = sw128(t, 4 * half + c);
             const uint4 gv = *reinterpret_cast<const uint4 *>(sm.go + at), vv = *reinterpret_cast<const uint4 *>(sm.v + at);
-            const float2 e2 = f2(e), w2 = f2(w);
+            const float2 e2 = f2(hd.e), w2 = f2(hd.w);
             *reinterpret_cast<uint4 *>(sm.gs + at) = make_uint4(pack2(mul2(unpack2(gv.x), e2)), pack2(mul2(unpack2(gv.y), e2)), pack2(mul2(unpack2(gv.z), e2)), pack2(mul2(unpack2(gv.w), e2)));
             *reinterpret_cast<uint4 *>(sm.vs + at) = make_uint4(pack2(mul2(unpack2(vv.x), w2)), pack2(mul2(unpack2(vv.y), w2)), pack2(mul2(unpack2(vv.z), w2)), pack2(mul2(unpack2(vv.w), w2)));
             dd = dot_bf16(unpack2(gv.x), vv.x, dot_bf16(unpack2(gv.y), vv.y, dot_bf16(unpack2(gv.z), vv.z, dot_bf16(unpack2(gv.w), vv.w, dd))));
         }
-        split_state<N>(sm, S);
         fence_async_smem();
-        mbar_arrive(&sm.bar[B_A]);
+        mbar_arrive(&sm.bar[B_SCALED]);
         load_state(G, state_at(p.dstates, it));
-        // -- M, the sum over heads, and the sums of R
-        if (!(ok = wait(B_A, it) && wait(B_DX, it))) break;   // (everybody's a2 and r, too)
+        if (sl == 0 && it > 0 && !(ok = finish(i - 1, old_a, old_dt, old_whole))) break;
+        // -- x
+        if (!(ok = wait(B_QS, it))) break;
         tc_fence_after();
+        {
+            float u[16], y[16], s = 0.f;
+            tmem_ld16x2(tm + TM_SG + half * 32, tm + TM_SG + half * 32 + 16, u, y);
+            tc_fence_before();
+            mbar_arrive(&sm.bar[B_X]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint4 gv = *piece(sm.go, t, 4 * half + c);
+                const float *q = c < 2 ? u + 8 * c : y + 8 * (c - 2);
+                s = dot_bf16(f2(q[0], q[1]), gv.x, dot_bf16(f2(q[2], q[3]), gv.y, dot_bf16(f2(q[4], q[5]), gv.z, dot_bf16(f2(q[6], q[7]), gv.w, s))));
+            }
+            x = fmaf(hd.e, s, x);
+        }
+        // -- parts of G
+        if (row)
+#pragma unroll
+            for (int c = 0; c < HS / 2; ++c) sg = fmaf(S[c].x, G[c].x, fmaf(S[c].y, G[c].y, sg));
+        if (!(ok = wait(B_DQ, it))) break;
+        split_state<N>(sm, G);
+        fence_async_smem();
+        mbar_arrive(&sm.bar[B_G]);
+        if (it + 1 < wk.items) load_state(S, state_at(p.states, it + 1));
+        // -- M, the sum over heads, and the sums of R
+        if (!(ok = wait(B_DX, it))) break;
+        tc_fence_after();
+        const float *rr_ = sm.r[i & 1], *aa = sm.a2[i & 1];
 #pragma unroll
         for (int ii = 0; ii < 2; ++ii) {
             const int I = 2 * half + ii;   // block of 32 columns i
@@ -204,82 +316,67 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
                     for (int y = 0; y < 8; ++y) mm[y] = f2(0.f);
                 } else {
                     float cb[16], dx[16];
-                    tmem_ld16(tm + TM_CB + I * 32 + u, cb);
-                    tmem_ld16(tm + TM_DX + I * 32 + u, dx);
-                    const float f = ii ? f1 : f0;
+                    tmem_ld16x2(tm + TM_CB + I * 32 + u, tm + TM_DX + I * 32 + u, cb, dx);
+                    const float2 f = f2(ii ? hd.f1 : hd.f0), dt2 = f2(hd.dt);
+                    float2 sum = f2(0.f);
 #pragma unroll
-                    for (int y = 0; y < 16; y += 2) {
-                        const int i = I * 32 + u + y;
-                        float2 L;
+                    for (int y = 0; y < 16; y += 4) {
+                        float2 L[2];
                         if (I > warp) {
-                            const float2 ri = *reinterpret_cast<const float2 *>(&sm.r[i]);
-                            L = mul2(ri, f2(f));
+                            const float4 ri = load4(rr_ + I * 32 + u + y);
+                            L[0] = mul2(f2(ri.x, ri.y), f);
+                            L[1] = mul2(f2(ri.z, ri.w), f);
                         } else {
-                            const float2 ai = *reinterpret_cast<const float2 *>(&sm.a2[i]);
-                            L.x = u + y >= lane ? ex2_approx(ai.x - a2) : 0.f;
-                            L.y = u + y + 1 >= lane ? ex2_approx(ai.y - a2) : 0.f;
+                            const float4 ai = load4(aa + I * 32 + u + y);
+                            L[0] = f2(u + y >= lane ? ex2_approx(ai.x - hd.a2) : 0.f, u + y + 1 >= lane ? ex2_approx(ai.y - hd.a2) : 0.f);
+                            L[1] = f2(u + y + 2 >= lane ? ex2_approx(ai.z - hd.a2) : 0.f, u + y + 3 >= lane ? ex2_approx(ai.w - hd.a2) : 0.f);
                         }
-                        const float2 d = f2(dx[y], dx[y + 1]), uu = mul2(L, f2(cb[y], cb[y + 1]));
-                        mm[y / 2] = mul2(uu, f2(dt_now));
-                        ms[ii * 16 + (u + y) / 2] = fma2(mul2(L, d), f2(dt_now), ms[ii * 16 + (u + y) / 2]);
-                        float2 rr = mul2(uu, d);
-                        c_all += rr.x + rr.y;
-                        if (I == warp) {
-                            if (u + y == lane) c_diag += rr.x, rr.x = 0.f;
-                            if (u + y + 1 == lane) c_diag += rr.y, rr.y = 0.f;
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const int c = y + 2 * k;
+                            const float2 d = f2(dx[c], dx[c + 1]), lc = mul2(L[k], f2(cb[c], cb[c + 1]));
+                            mm[c / 2] = mul2(lc, dt2);
+                            ms[ii * 16 + (u + c) / 2] = fma2(mul2(L[k], d), dt2, ms[ii * 16 + (u + c) / 2]);
+                            const float2 rr = mul2(lc, d);
+                            sum = add2(sum, rr);
+                            const float2 rd = mul2(rr, dt2);
+                            rs[u + c] = rd.x;
+                            rs[u + c + 1] = rd.y;
+                            if (I == warp) {   // not the diagonal: its decay is 1
+                                if (u + c == lane) c_diag += rr.x, rs[u + c] = 0.f;
+                                if (u + c + 1 == lane) c_diag += rr.y, rs[u + c + 1] = 0.f;
+                            }
                         }
-                        rs[u + y] = rr.x * dt_now;
-                        rs[u + y + 1] = rr.y * dt_now;
                     }
+                    c_all += sum.x + sum.y;
                 }
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
                     *piece(sm.m[half], t, ii * 4 + (u >> 3) + y) = make_uint4(pack2(mm[4 * y]), pack2(mm[4 * y + 1]), pack2(mm[4 * y + 2]), pack2(mm[4 * y + 3]));
+            }
+            if (ii == 1) {
+                fence_async_smem();
+                tc_fence_before();
+                mbar_arrive(&sm.bar[B_M]);
             }
             if (I >= warp) {
                 const float s = column_sums(rs);
                 sm.rows[warp][I * 32 + lane] = sl ? sm.rows[warp][I * 32 + lane] + s : s;
             }
         }
-        fence_async_smem();
-        tc_fence_before();
-        mbar_arrive(&sm.bar[B_M]);
-        // -- x, then the parts of G
-        if (!(ok = wait(B_C1, it))) break;
-        tc_fence_after();
-        {
-            float s = 0.f;
-#pragma unroll
-            for (int u = 0; u < 32; u += 16) {
-                float qs[16];
-                tmem_ld16(tm + TM_SG + half * 32 + u, qs);
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const uint4 gv = *piece(sm.go, t, 4 * half + (u >> 3) + y);
-                    s = dot_bf16(f2(qs[8 * y], qs[8 * y + 1]), gv.x, dot_bf16(f2(qs[8 * y + 2], qs[8 * y + 3]), gv.y, dot_bf16(f2(qs[8 * y + 4], qs[8 * y + 5]), gv.z, dot_bf16(f2(qs[8 * y + 6], qs[8 * y + 7]), gv.w, s))));
-                }
-            }
-            x = fmaf(e, s, x);
-        }
-        if (row)
-#pragma unroll
-            for (int i = 0; i < HS / 2; ++i) sg = fmaf(S[i].x, G[i].x, fmaf(S[i].y, G[i].y, sg));
-        split_state<N>(sm, G);
-        fence_async_smem();
-        tc_fence_before();
-        mbar_arrive(&sm.bar[B_B]);
-        if (it + 1 < wk.items) load_state(S, state_at(p.states, it + 1));
+        // -- the next head's decays, while M do and k G are formed
+        const bool last = sl == slices - 1;
+        if (last && i + 1 < heads && !(ok = decays(i + 1, next))) break;
         // -- dv and z
         if (!(ok = wait(B_C2, it))) break;
         tc_fence_after();
         {
-            const float2 skip = f2(p.a.skip ? p.a.skip[h] : 0.f), w2 = f2(w);
+            const float2 skip = f2(p.a.skip ? p.a.skip[h] : 0.f), w2 = f2(hd.w);
             float s = 0.f;
 #pragma unroll
             for (int u = 0; u < 32; u += 16) {
                 float kg[16], dv[16];
-                tmem_ld16(tm + TM_SG + half * 32 + u, kg);
-                tmem_ld16(tm + TM_DV + half * 32 + u, dv);
+                tmem_ld16x2(tm + TM_SG + half * 32 + u, tm + TM_DV + half * 32 + u, kg, dv);
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const uint4 vv = *piece(sm.v, t, 4 * half + (u >> 3) + y), gv = *piece(sm.go, t, 4 * half + (u >> 3) + y);
@@ -297,71 +394,32 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
             z += s;   // (without w_j)
         }
         tc_fence_before();
+        mbar_arrive(&sm.bar[B_FREE]);
         __syncwarp();
         {
-            __nv_bfloat16 *dv = static_cast<__nv_bfloat16 *>(p.a.dv) + ((size_t)wk.tok0 * p.a.H + h) * p.a.P + sl * NS + half * 32 + (lane & 3) * 8;
+            __nv_bfloat16 *dv = static_cast<__nv_bfloat16 *>(p.a.dv) + ((size_t)(wk.tok0 + warp * 32 + (lane >> 2)) * p.a.H + h) * p.a.P + sl * NS + half * 32 + (lane & 3) * 8;
+            const int rr = warp * 32 + (lane >> 2);
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-                const int rr = warp * 32 + i + (lane >> 2);
-                if (rr < m) *reinterpret_cast<uint4 *>(dv + (size_t)rr * p.a.H * p.a.P) = *piece(sm.gs, rr, 4 * half + (lane & 3));
-            }
+            for (int c = 0; c < 32; c += 8)
+                if (rr + c < m) *reinterpret_cast<uint4 *>(dv + (size_t)c * p.a.H * p.a.P) = *piece(sm.gs, rr + c, 4 * half + (lane & 3));
         }
         __syncwarp();
-        mbar_arrive(&sm.bar[B_FREE]);
-        // -- gradients of dt and a, behind a head's last slice
-        if (sl == slices - 1) {
-            sm.acc[half][0][t] = x - dt_now * (c_all - c_diag);
-            sm.acc[half][1][t] = w * z;
-            sm.acc[half][2][t] = fmaf(wn, z, c_all);
+        if (last) {
+            sm.acc[half][0][t] = x - hd.dt * (c_all - c_diag);
+            sm.acc[half][1][t] = hd.w * z;
+            sm.acc[half][2][t] = fmaf(hd.wn, z, c_all);
             sm.acc[half][3][t] = dd;
             for (int o = 16; o > 0; o >>= 1) sg += __shfl_xor_sync(0xffffffffu, sg, o);
             if (lane == 0) sm.sg[threadIdx.x >> 5] = sg;
             mbar_arrive(&sm.bar[B_E]);
-            if (!(ok = wait(B_E, it / slices))) break;
-            if (half == 0) {   // a warp to 32 tokens; of the others' it needs the sums
-                float all = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) all += sm.sg[i];
-                float later = 0.f, earlier = 0.f, own = 0.f, zt = 0.f;
-#pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const int i = b * 32 + lane;
-                    float o = 0.f, y = 0.f;
-                    if (b >= warp) {
-                        o = sm.acc[0][0][i] + sm.acc[1][0][i];
-#pragma unroll
-                        for (int J = 0; J <= b; ++J) o += sm.rows[J][i];
-                    }
-                    if (b <= warp) y = sm.acc[0][1][i] + sm.acc[1][1][i];
-                    if (b > warp) later += o;
-                    if (b == warp) own = o, zt = y;
-                    if (b < warp) earlier += y;
-                }
-                float suffix = own, prefix = zt;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const float u = __shfl_down_sync(0xffffffffu, suffix, o), y = __shfl_up_sync(0xffffffffu, prefix, o);
-                    if (lane + o < 32) suffix += u;
-                    if (lane >= o) prefix += y;
-                    later += __shfl_xor_sync(0xffffffffu, later, o);
-                    earlier += __shfl_xor_sync(0xffffffffu, earlier, o);
-                }
-                const float before = __shfl_up_sync(0xffffffffu, prefix, 1);
-                const float F = suffix + later + (lane ? before : 0.f) + earlier + whole * all;
-                if (in) p.a.ddt[row_out * p.a.H + h] = fmaf(a, F, sm.acc[0][2][t] + sm.acc[1][2][t]);
-                float da = in ? dt_now * F : 0.f, d = sm.acc[0][3][t] + sm.acc[1][3][t];
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) {
-                    da += __shfl_xor_sync(0xffffffffu, da, o);
-                    d += __shfl_xor_sync(0xffffffffu, d, o);
-                }
-                if (lane == 0) {
-                    p.part_a[((size_t)wk.slot * 4 + warp) * p.a.H + h] = da;
-                    p.part_d[((size_t)wk.slot * 4 + warp) * p.a.H + h] = d;
-                }
-            }
+            old_a = hd.a;
+            old_dt = hd.dt;
+            old_whole = hd.whole;
+            hd = next;
+            c_all = c_diag = z = x = dd = sg = 0.f;
         }
     }
+    ok = ok && finish(heads - 1, old_a, old_dt, old_whole);
     if (!ok || sm.abort_flag) return;
     // -- the heads' sum as an operand, row j
 #pragma unroll
@@ -443,29 +501,30 @@ __device__ void issue(Smem &sm, const CUtensorMap *tq, const CUtensorMap *tk, co
     mma_commit(&sm.bar[B_CB]);
 #pragma unroll 1
     for (int it = 0; it < wk.items; ++it) {
-        if (it > 0) {
+        if (it > 0) {   // (the tiles and accumulators of the last slice have been read)
             if (!wait(B_FREE, it - 1)) return;
             load(it);
         }
-        if (!wait(B_TILES, it) || (wk.m < C && !wait(B_CLEAN, it))) return;
-        mma4_bf16_lo<2, 2>(tm + TM_DX, v_km, go_km, idesc_bf16(128, 128, 0, 0), 0);
-        mma_commit(&sm.bar[B_DX]);
-        if (!wait(B_A, it)) return;
-        mma4_bf16_lo<2, 2>(tm + TM_DQ, gs_km, sp_km + T16, idesc_bf16(128, N, 0, 0), it > 0);
-        mma4_bf16_lo<2, 2>(tm + TM_DQ, gs_km, sp_km, idesc_bf16(128, N, 0, 0), 1);
-        if (!wait(B_M, it)) return;
+        if (!wait(B_S, it)) return;
 #pragma unroll 1
         for (int part = 2; part >= 0; --part)   // smallest first
 #pragma unroll
             for (int b = 0; b < NB; ++b) mma4_bf16_lo<2, 128>(tm + TM_SG, q_km + b * T16, sp_km + part * T16 + b * 512, idesc_bf16(128, 64, 0, 1), part < 2 || b > 0);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) mma4_bf16_lo<2, 128>(tm + TM_DV, m_km + b * T16, go_km + b * 512, idesc_bf16(128, 64, 0, 1), b);
-        mma_commit(&sm.bar[B_C1]);
-        if (!wait(B_B, it)) return;
+        mma_commit(&sm.bar[B_QS]);
+        if (!wait(B_SCALED, it)) return;
+        mma4_bf16_lo<2, 2>(tm + TM_DQ, gs_km, sp_km + T16, idesc_bf16(128, N, 0, 0), it > 0);
+        mma4_bf16_lo<2, 2>(tm + TM_DQ, gs_km, sp_km, idesc_bf16(128, N, 0, 0), 1);
+        mma_commit(&sm.bar[B_DQ]);
+        if (!wait(B_TILES, it) || (wk.m < C && !wait(B_CLEAN, it)) || !wait(B_X, it)) return;
+        mma4_bf16_lo<2, 2>(tm + TM_DX, v_km, go_km, idesc_bf16(128, 128, 0, 0), 0);
+        mma_commit(&sm.bar[B_DX]);
+        if (!wait(B_G, it) || !wait(B_M, it)) return;
 #pragma unroll 1
         for (int part = 2; part >= 0; --part)
 #pragma unroll
             for (int b = 0; b < NB; ++b) mma4_bf16_lo<2, 128>(tm + TM_SG, k_km + b * T16, sp_km + part * T16 + b * 512, idesc_bf16(128, 64, 0, 1), part < 2 || b > 0);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) mma4_bf16_lo<2, 128>(tm + TM_DV, m_km + b * T16, go_km + b * 512, idesc_bf16(128, 64, 0, 1), b);
         mma4_bf16_lo<2, 2>(tm + TM_DK, vs_km, sp_km + T16, idesc_bf16(128, N, 0, 0), it > 0);
         mma4_bf16_lo<2, 2>(tm + TM_DK, vs_km, sp_km, idesc_bf16(128, N, 0, 0), 1);
         if (p.a.test_timeout) return;   // test hook: the workers' wait for these products runs out
@@ -515,7 +574,7 @@ ssm_grads_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constan
     }
     if (tid == 0) {
         for (int b = 0; b < B_COUNT; ++b)
-            mbar_init(&sm.bar[b], b == B_TOT ? 8 : b == B_CLEAN0 || b == B_CLEAN || b == B_A || b == B_M || b == B_B || b == B_E || b == B_FREE || b == B_MS ? 256 : 1);
+            mbar_init(&sm.bar[b], b == B_TOT ? 8 : b > B_TOT ? 256 : 1);
         sm.abort_flag = 0;
         mbar_fence_init();
         tma_prefetch_desc(&tq);
