@@ -28,7 +28,7 @@ constexpr int NT = 256 + 128;   // (of the last warpgroup one warp works)
 enum Bar {
     B_QK = 0,       // q and k landed
     B_TILES,        // v and do landed
-    B_CB, B_QS, B_DQ, B_DX, B_C2, B_FIN,   // products complete: k q^T; q S; its share of dq; DX^T; M do, k G and dk's share; the last ones
+    B_CB, B_QS, B_DQ, B_DX, B_C2, B_DK, B_FIN,   // products complete: k q^T; q S; its share of dq; DX^T; M do and k G; dk's share; the last ones
     B_TOT,          // sums over 32 tokens written (a warp)
     B_CLEAN0, B_CLEAN,   // rows behind the sequence's end zeroed: of q and k, of v and do (all workers, like those below)
     B_S, B_SCALED, B_X, B_G, B_M,   // written: parts of S; scaled tiles; x read; parts of G; M
@@ -48,10 +48,11 @@ struct Smem {
     alignas(1024) unsigned char m[2][TILE];               // M^T, at the end the sum over heads: [64 of i][j][64]
     alignas(1024) unsigned char gs[TILE], vs[TILE];       // e^{l_i} do, w_j v
     float a2[2][C], r[2][C];  // of heads in turn
-    float rows[4][C];         // sums over 32 tokens j of R_ij, j < i
-    float acc[2][4][C];       // of a token, by half of the columns: its own share of F (but for the sums of rows), z, what ddt has directly, do . v
+    // of heads in turn:
+    float rows[2][4][C];      // sums over 32 tokens j of R_ij
+    float acc[2][2][4][C];    // of a token, by half of the columns: its own share of F (but for the sums of rows), z, what ddt has directly, do . v
     float tot[2][4];
-    float sg[8];
+    float sg[2][8];
     alignas(8) uint64_t bar[B_COUNT];
     uint32_t tmem;
     volatile int abort_flag;
@@ -169,10 +170,9 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
     float2 S[HS / 2], G[HS / 2];
     load_state(S, state_at(p.states, 0));
     const int heads = wk.items / slices;
-    float next_dt = in ? p.a.dt[row_out * p.a.H + wk.h0] : 0.f;
+    float next_dt = in ? p.a.dt[row_out * p.a.H + wk.h0] : 0.f, next_a = p.a.a[wk.h0];
     auto decays = [&](int i, Head &hd) {   // of the i-th head
-        const int h = wk.h0 + i;
-        hd.a = p.a.a[h];
+        hd.a = next_a;
         hd.dt = next_dt;
         const BlockScan b(hd.dt, hd.a);
         float *tot = sm.tot[i & 1];
@@ -184,7 +184,6 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         const float r = exp2f(b.a2);
         if (half == 0) sm.a2[i & 1][t] = b.a2;
         else sm.r[i & 1][t] = r;
-        if (i + 1 < heads) next_dt = in ? p.a.dt[row_out * p.a.H + h + 1] : 0.f;
         if (!wait(B_TOT, i)) return false;
         const float t0 = tot[0], t1 = tot[1], t2 = tot[2], t3 = tot[3];
         hd.e = r * exp2f(warp == 0 ? 0.f : warp == 1 ? t0 : warp == 2 ? t0 + t1 : t0 + t1 + t2);
@@ -200,24 +199,25 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         if (!wait(B_E, i)) return false;
         if (half) return true;
         const int h = wk.h0 + i;
+        const auto &acc = sm.acc[i & 1];
         float all = 0.f, later = 0.f, earlier = 0.f, own = 0.f, zt = 0.f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) all += sm.sg[k];
+        for (int k = 0; k < 8; ++k) all += sm.sg[i & 1][k];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             const int at = b * 32 + lane;
             float o = 0.f, y = 0.f;
             if (b >= warp) {
-                o = sm.acc[0][0][at] + sm.acc[1][0][at];
+                o = acc[0][0][at] + acc[1][0][at];
 #pragma unroll
-                for (int J = 0; J <= b; ++J) o += sm.rows[J][at];
+                for (int J = 0; J <= b; ++J) o += sm.rows[i & 1][J][at];
             }
-            if (b <= warp) y = sm.acc[0][1][at] + sm.acc[1][1][at];
+            if (b <= warp) y = acc[0][1][at] + acc[1][1][at];
             if (b > warp) later += o;
             if (b == warp) own = o, zt = y;
             if (b < warp) earlier += y;
         }
-        float suffix = own, prefix = zt, d = sm.acc[0][3][t] + sm.acc[1][3][t];
+        float suffix = own, prefix = zt, d = acc[0][3][t] + acc[1][3][t];
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const float u = __shfl_down_sync(0xffffffffu, suffix, o), y = __shfl_up_sync(0xffffffffu, prefix, o);
@@ -228,7 +228,7 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         }
         const float before = __shfl_up_sync(0xffffffffu, prefix, 1);
         const float F = suffix + later + (lane ? before : 0.f) + earlier + whole * all;
-        if (in) p.a.ddt[row_out * p.a.H + h] = fmaf(a, F, sm.acc[0][2][t] + sm.acc[1][2][t]);
+        if (in) p.a.ddt[row_out * p.a.H + h] = fmaf(a, F, acc[0][2][t] + acc[1][2][t]);
         float da = in ? dt * F : 0.f;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
@@ -242,13 +242,18 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         return true;
     };
     Head hd, next;
-    float c_all = 0.f, c_diag = 0.f, z = 0.f, x = 0.f, dd = 0.f, sg = 0.f;   // sums over a head's slices
+    float c_all = 0.f, z = 0.f, x = 0.f, dd = 0.f, sg = 0.f;   // sums over a head's slices
     float old_a = 0.f, old_dt = 0.f, old_whole = 0.f;                        // of the head before
     bool ok = decays(0, hd) && wait(B_CB, 0);
 #pragma unroll 1
     for (int it = 0; ok && it < wk.items; ++it) {
         const int i = it / slices, h = wk.h0 + i, sl = it % slices;
+        if (sl == 0 && i + 1 < heads) {   // (needed while this head's last product runs)
+            next_dt = in ? p.a.dt[row_out * p.a.H + h + 1] : 0.f;
+            next_a = p.a.a[h + 1];
+        }
         // -- parts of S
+        if (it > 0 && !(ok = wait(B_DK, it - 1))) break;
         split_state<N>(sm, S);
         fence_async_smem();
         mbar_arrive(&sm.bar[B_S]);
@@ -269,12 +274,10 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
             const float2 e2 = f2(hd.e), w2 = f2(hd.w);
             *reinterpret_cast<uint4 *>(sm.gs + at) = make_uint4(pack2(mul2(unpack2(gv.x), e2)), pack2(mul2(unpack2(gv.y), e2)), pack2(mul2(unpack2(gv.z), e2)), pack2(mul2(unpack2(gv.w), e2)));
             *reinterpret_cast<uint4 *>(sm.vs + at) = make_uint4(pack2(mul2(unpack2(vv.x), w2)), pack2(mul2(unpack2(vv.y), w2)), pack2(mul2(unpack2(vv.z), w2)), pack2(mul2(unpack2(vv.w), w2)));
-            dd = dot_bf16(unpack2(gv.x), vv.x, dot_bf16(unpack2(gv.y), vv.y, dot_bf16(unpack2(gv.z), vv.z, dot_bf16(unpack2(gv.w), vv.w, dd))));
         }
         fence_async_smem();
         mbar_arrive(&sm.bar[B_SCALED]);
         load_state(G, state_at(p.dstates, it));
-        if (sl == 0 && it > 0 && !(ok = finish(i - 1, old_a, old_dt, old_whole))) break;
         // -- x
         if (!(ok = wait(B_QS, it))) break;
         tc_fence_after();
@@ -299,7 +302,6 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         split_state<N>(sm, G);
         fence_async_smem();
         mbar_arrive(&sm.bar[B_G]);
-        if (it + 1 < wk.items) load_state(S, state_at(p.states, it + 1));
         // -- M, the sum over heads, and the sums of R
         if (!(ok = wait(B_DX, it))) break;
         tc_fence_after();
@@ -342,10 +344,6 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
                             const float2 rd = mul2(rr, dt2);
                             rs[u + c] = rd.x;
                             rs[u + c + 1] = rd.y;
-                            if (I == warp) {   // not the diagonal: its decay is 1
-                                if (u + c == lane) c_diag += rr.x, rs[u + c] = 0.f;
-                                if (u + c + 1 == lane) c_diag += rr.y, rs[u + c + 1] = 0.f;
-                            }
                         }
                     }
                     c_all += sum.x + sum.y;
@@ -361,12 +359,15 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
             }
             if (I >= warp) {
                 const float s = column_sums(rs);
-                sm.rows[warp][I * 32 + lane] = sl ? sm.rows[warp][I * 32 + lane] + s : s;
+                float &to = sm.rows[i & 1][warp][I * 32 + lane];
+                to = sl ? to + s : s;
             }
         }
-        // -- the next head's decays, while M do and k G are formed
+        if (it + 1 < wk.items) load_state(S, state_at(p.states, it + 1));   // (from L2; not before the sums of R, which need the registers)
+        // -- the next head's decays and the last one's gradients, while M do and k G are formed
         const bool last = sl == slices - 1;
         if (last && i + 1 < heads && !(ok = decays(i + 1, next))) break;
+        if (last && i > 0 && !(ok = finish(i - 1, old_a, old_dt, old_whole))) break;
         // -- dv and z
         if (!(ok = wait(B_C2, it))) break;
         tc_fence_after();
@@ -386,6 +387,7 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
                     for (int q = 0; q < 4; ++q) {
                         const float2 kk = f2(kg[8 * y + 2 * q], kg[8 * y + 2 * q + 1]);
                         s = dot_bf16(kk, vw[q], s);
+                        dd = dot_bf16(unpack2(gw[q]), vw[q], dd);
                         o[q] = pack2(fma2(skip, unpack2(gw[q]), fma2(w2, kk, f2(dv[8 * y + 2 * q], dv[8 * y + 2 * q + 1]))));
                     }
                     *piece(sm.gs, t, 4 * half + (u >> 3) + y) = make_uint4(o[0], o[1], o[2], o[3]);   // (read by the products that have completed)
@@ -405,18 +407,18 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         }
         __syncwarp();
         if (last) {
-            sm.acc[half][0][t] = x - hd.dt * (c_all - c_diag);
-            sm.acc[half][1][t] = hd.w * z;
-            sm.acc[half][2][t] = fmaf(hd.wn, z, c_all);
-            sm.acc[half][3][t] = dd;
+            sm.acc[i & 1][half][0][t] = x - hd.dt * c_all;   // (R_tt cancels)
+            sm.acc[i & 1][half][1][t] = hd.w * z;
+            sm.acc[i & 1][half][2][t] = fmaf(hd.wn, z, c_all);
+            sm.acc[i & 1][half][3][t] = dd;
             for (int o = 16; o > 0; o >>= 1) sg += __shfl_xor_sync(0xffffffffu, sg, o);
-            if (lane == 0) sm.sg[threadIdx.x >> 5] = sg;
+            if (lane == 0) sm.sg[i & 1][threadIdx.x >> 5] = sg;
             mbar_arrive(&sm.bar[B_E]);
             old_a = hd.a;
             old_dt = hd.dt;
             old_whole = hd.whole;
             hd = next;
-            c_all = c_diag = z = x = dd = sg = 0.f;
+            c_all = z = x = dd = sg = 0.f;
         }
     }
     ok = ok && finish(heads - 1, old_a, old_dt, old_whole);
@@ -492,7 +494,18 @@ __device__ void issue(Smem &sm, const CUtensorMap *tq, const CUtensorMap *tk, co
         }
         __syncwarp();
     };
+    // States on their way to L2, two slices ahead.
+    auto fetch = [&](int it) {
+        if (first && it < wk.items) {
+            const size_t at = (((size_t)wk.slot * p.a.H + wk.h0) * slices + it) * STATE_ELEMS;
+            prefetch_l2(p.states + at, STATE_ELEMS * 4);
+            prefetch_l2(p.dstates + at, STATE_ELEMS * 4);
+        }
+        __syncwarp();
+    };
     load(0);
+    fetch(0);
+    fetch(1);
     if (!wait(B_QK, 0) || (wk.m < C && !wait(B_CLEAN0, 0))) return;
     const uint32_t k_km = desc(sm.k, 0), q_km = desc(sm.q, 0), v_km = desc(sm.v, 0), go_km = desc(sm.go, 0), gs_km = desc(sm.gs, 0), vs_km = desc(sm.vs, 0);
     const uint32_t sp_km = desc(sm.sp, 0), m_km = desc(sm.m, 0), m_mn = desc(sm.m, TILE), k_mn = desc(sm.k, TILE), q_mn = desc(sm.q, TILE);
@@ -505,6 +518,7 @@ __device__ void issue(Smem &sm, const CUtensorMap *tq, const CUtensorMap *tk, co
             if (!wait(B_FREE, it - 1)) return;
             load(it);
         }
+        fetch(it + 2);
         if (!wait(B_S, it)) return;
 #pragma unroll 1
         for (int part = 2; part >= 0; --part)   // smallest first
@@ -525,10 +539,11 @@ __device__ void issue(Smem &sm, const CUtensorMap *tq, const CUtensorMap *tk, co
             for (int b = 0; b < NB; ++b) mma4_bf16_lo<2, 128>(tm + TM_SG, k_km + b * T16, sp_km + part * T16 + b * 512, idesc_bf16(128, 64, 0, 1), part < 2 || b > 0);
 #pragma unroll
         for (int b = 0; b < 2; ++b) mma4_bf16_lo<2, 128>(tm + TM_DV, m_km + b * T16, go_km + b * 512, idesc_bf16(128, 64, 0, 1), b);
-        mma4_bf16_lo<2, 2>(tm + TM_DK, vs_km, sp_km + T16, idesc_bf16(128, N, 0, 0), it > 0);
-        mma4_bf16_lo<2, 2>(tm + TM_DK, vs_km, sp_km, idesc_bf16(128, N, 0, 0), 1);
         if (p.a.test_timeout) return;   // test hook: the workers' wait for these products runs out
         mma_commit(&sm.bar[B_C2]);
+        mma4_bf16_lo<2, 2>(tm + TM_DK, vs_km, sp_km + T16, idesc_bf16(128, N, 0, 0), it > 0);
+        mma4_bf16_lo<2, 2>(tm + TM_DK, vs_km, sp_km, idesc_bf16(128, N, 0, 0), 1);
+        mma_commit(&sm.bar[B_DK]);
     }
     if (!wait(B_MS, 0)) return;
 #pragma unroll

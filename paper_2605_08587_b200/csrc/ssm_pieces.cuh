@@ -44,6 +44,10 @@ __device__ __forceinline__ void prefetch_2d(const void *tmap, int x, int y)
     asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(tmap), "r"(x), "r"(y) : "memory");
 }
 
+__device__ __forceinline__ void prefetch_l2(const void *x, int bytes)   // (multiples of 16)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(x), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void prefetch_line(const void *x) { asm volatile("prefetch.global.L2 [%0];" ::"l"(x)); }
 
 // Few long sequences are cut into parts of whole chunks.
