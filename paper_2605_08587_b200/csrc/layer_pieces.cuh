@@ -107,8 +107,20 @@ struct Sequences {
     }
 };
 
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_fast(float x)   // off by at most one in the last place; 0 beyond 2^126
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // 1 / (1 + exp(-x)).  exp overflows to infinity for x < -88 and the quotient is then 0, as it should be.
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+__device__ __forceinline__ float sigmoid(float x) { return rcp_fast(1.f + exp2_fast(x * -1.4426950408889634f)); }
 
 // Sums of n partials [n][M] in a fixed order: a block takes 32 columns, each of its 16 warps every 16th partial; store(i, sum).
 template <typename F>
@@ -117,8 +129,17 @@ __device__ __forceinline__ void sum_partials(const float *partial, int n, int M,
     __shared__ float part[16][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
     float s = 0.f;
-    if (i < M)
-        for (int k = warp; k < n; k += 16) s += partial[(size_t)k * M + i];
+    if (i < M) {
+        int k = warp;
+        for (; k + 112 < n; k += 128) {   // eight in flight
+            float x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = partial[(size_t)(k + 16 * u) * M + i];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += x[u];
+        }
+        for (; k < n; k += 16) s += partial[(size_t)k * M + i];
+    }
     part[warp][lane] = s;
     __syncthreads();
     if (warp == 0 && i < M) {

@@ -393,7 +393,7 @@ static int norm_mode(const NormParams &p) { return p.residual ? NORM_ADD : p.gat
 // Blocks of the backward's persistent grid (each leaves one partial), and the row runs of the column sums of any width.
 static int bwd_blocks(int rows, const NormShape &s)
 {
-    const int per_sm = 1024 / (s.tx * s.ty) > 0 ? 1024 / (s.tx * s.ty) : 1;
+    const int per_sm = 512 / (s.tx * s.ty) > 0 ? 512 / (s.tx * s.ty) : 1;   // (as many as are resident: fewer partial sums)
     const int need = ceil_div(rows, s.ty), most = per_sm * sm_count();
     return need < 1 ? 1 : need < most ? need : most;
 }
