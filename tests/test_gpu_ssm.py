@@ -12,7 +12,9 @@ import pytest
 import torch
 
 from layer_refs import check, grads, leaf, scan
-from paper_2605_08587_b200 import KLA_FLAG_FORCE_SIMT, KLA_FLAG_NO_SEGMENTS, KLA_FLAG_NONE, kla_ssm_bwd, kla_ssm_fwd, kla_ssm_step, launch_count
+from paper_2605_08587_b200 import (KLA_FLAG_FORCE_SIMT, KLA_FLAG_NO_SEGMENTS, KLA_FLAG_NONE, KlaError, check as check_status, kla_ssm_bwd, kla_ssm_fwd,
+                                   kla_ssm_step, launch_count)
+from paper_2605_08587_b200.binding import KLA_INTERNAL_FLAG_TEST_TIMEOUT
 
 DEV = "cuda:0"
 BF, F32 = torch.bfloat16, torch.float32
@@ -231,3 +233,39 @@ def test_results_do_not_vary():
         y2, f2 = kla_ssm_fwd(*args, **more)
         g2 = kla_ssm_bwd(*args, dy, d_final_state=df, **more)
         assert torch.equal(y, y2) and torch.equal(f, f2) and all(torch.equal(g[n], g2[n]) for n in g)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens, H, G, N, P", [([2000], 1, 1, 128, 64), ([0, 1700, 129], 2, 1, 64, 64), ([1300, 0], 1, 1, 64, 128)])
+def test_backward_of_long_sequences_in_parts(lens, H, G, N, P):
+    """Against the fp32 kernels on CUDA cores (each bf16 gradient has one rounding of its own and one of its operands; fp32 sums over T, N and P)."""
+    s, seqs, dy, df = make(lens, H, G, N, P, BF, seed=11)
+    args = [s[n] for n in ("q", "k", "v", "dt", "a")]
+    more = dict(d_skip=s["d_skip"], init_state=s["init_state"], d_final_state=df, **seqs)
+    g, r = kla_ssm_bwd(*args, dy, **more), kla_ssm_bwd(*args, dy, flags=KLA_FLAG_FORCE_SIMT, **more)
+    whole = kla_ssm_bwd(*args, dy, flags=KLA_FLAG_NO_SEGMENTS, **more)
+    for n in r:
+        for got in (g[n], whole[n]):
+            off = float((got.double() - r[n].double()).norm() / r[n].double().norm())
+            assert off <= (2.0 ** -7 if n in ("dq", "dk", "dv") else 2.0 ** -15), (n, off)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N, P", [(128, 64), (64, 128)])
+def test_a_wait_that_runs_out_is_reported(N, P):
+    """A completion that is withheld: the block gives up after about a second, says so, and the context stays usable."""
+    s, seqs, dy, _ = make([200], 1, 1, N, P, BF)
+    args = [s[n] for n in ("q", "k", "v", "dt", "a")]
+    word = torch.zeros(1, dtype=torch.int32, device=DEV)
+    kla_ssm_fwd(*args, flags=KLA_INTERNAL_FLAG_TEST_TIMEOUT, status_word=word, **seqs)
+    assert int(word) == -10
+    word.zero_()
+    kla_ssm_bwd(*args, dy, flags=KLA_INTERNAL_FLAG_TEST_TIMEOUT, status_word=word, **seqs)
+    assert int(word) == -10
+    kla_ssm_fwd(*args, flags=KLA_INTERNAL_FLAG_TEST_TIMEOUT, **seqs)   # the binding's own word
+    with pytest.raises(KlaError):
+        check_status()
+    check_status()
+    y, _ = kla_ssm_fwd(*args, **seqs)
+    y1, _ = kla_ssm_fwd(*args, flags=KLA_FLAG_FORCE_SIMT, **seqs)
+    assert float((y.double() - y1.double()).norm() / y1.double().norm()) <= 2.0 ** -8
