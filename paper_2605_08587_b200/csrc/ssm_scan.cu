@@ -44,7 +44,7 @@ template <typename IO, typename OUT, int R>
 __global__ void __launch_bounds__(128) ssm_scan_kernel(SsmParams p, Sequences seqs)
 {
     __shared__ __align__(16) float ks[TT][8 * R], qs[TT][8 * R];
-    __shared__ float vs[TT][16], al[TT], dts[TT];
+    __shared__ float vs[TT][16], al[TT];
     const int cols = (p.P + 15) / 16;
     const int cb = blockIdx.x % cols, h = blockIdx.x / cols % p.H, n = blockIdx.x / cols / p.H, g = h / (p.H / p.G);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = lane >> 2, cc = warp * 4 + (lane & 3), col = cb * 16 + cc;
@@ -59,42 +59,74 @@ __global__ void __launch_bounds__(128) ssm_scan_kernel(SsmParams p, Sequences se
     const IO *q = static_cast<const IO *>(p.q) + g * p.N, *k = static_cast<const IO *>(p.k) + g * p.N, *v = static_cast<const IO *>(p.v) + h * p.P;
     OUT *out = static_cast<OUT *>(p.out) + h * p.P + col;
     const float a = p.a[h], skip = p.skip ? p.skip[h] : 0.f;
+    // The next tile's operands wait in registers while this one's tokens run.
+    float nq[R], nk[R], nv[2], nd = 0.f;
+    auto fetch = [&](int t0) {
+        const int m = end - t0;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int i = threadIdx.x + 128 * j, t = i / (8 * R), x = i % (8 * R);
+            nq[j] = nk[j] = 0.f;
+            if (t < m && x < p.N) {
+                nq[j] = to_f32(q[(size_t)(t0 + t) * p.q_stride + x]);
+                nk[j] = to_f32(k[(size_t)(t0 + t) * p.k_stride + x]) * p.dt[(size_t)(t0 + t) * p.H + h];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int i = threadIdx.x + 128 * j, t = i >> 4, c = cb * 16 + (i & 15);
+            nv[j] = t < m && c < p.P ? to_f32(v[(size_t)(t0 + t) * p.v_stride + c]) : 0.f;
+        }
+        if (threadIdx.x < TT) nd = threadIdx.x < m ? p.dt[(size_t)(t0 + threadIdx.x) * p.H + h] : 0.f;
+    };
+    if (start < end) fetch(start);
     for (int t0 = start; t0 < end; t0 += TT) {
         const int m = min(TT, end - t0);
         __syncthreads();
-        if (threadIdx.x < TT) {
-            const float d = threadIdx.x < m ? p.dt[(size_t)(t0 + threadIdx.x) * p.H + h] : 0.f;
-            dts[threadIdx.x] = d;
-            al[threadIdx.x] = expf(d * a);
-        }
-        for (int i = threadIdx.x; i < TT * 16; i += 128) {
-            const int t = i >> 4, c = cb * 16 + (i & 15);
-            vs[t][i & 15] = t < m && c < p.P ? to_f32(v[(size_t)(t0 + t) * p.v_stride + c]) : 0.f;
-        }
-        SsmTile<IO>::template load<R>(qs, q, p.q_stride, t0, m, p.N, nullptr);
-        __syncthreads();
-        SsmTile<IO>::template load<R>(ks, k, p.k_stride, t0, m, p.N, dts);
-        __syncthreads();
-        for (int t = 0; t < m; ++t) {
-            const float x = vs[t][cc], d = al[t];
-            float y0 = 0.f, y1 = 0.f;
 #pragma unroll
-            for (int r = 0; r < R; r += 4) {
-                const float4 kk = *reinterpret_cast<const float4 *>(&ks[t][(r >> 2) * 32 + part * 4]);
-                const float4 qq = *reinterpret_cast<const float4 *>(&qs[t][(r >> 2) * 32 + part * 4]);
-                s[r] = fmaf(kk.x, x, d * s[r]);
-                s[r + 1] = fmaf(kk.y, x, d * s[r + 1]);
-                s[r + 2] = fmaf(kk.z, x, d * s[r + 2]);
-                s[r + 3] = fmaf(kk.w, x, d * s[r + 3]);
-                y0 = fmaf(qq.x, s[r], y0);
-                y1 = fmaf(qq.y, s[r + 1], y1);
-                y0 = fmaf(qq.z, s[r + 2], y0);
-                y1 = fmaf(qq.w, s[r + 3], y1);
+        for (int j = 0; j < R; ++j) {
+            const int i = threadIdx.x + 128 * j;
+            qs[i / (8 * R)][i % (8 * R)] = nq[j];
+            ks[i / (8 * R)][i % (8 * R)] = nk[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) vs[(threadIdx.x + 128 * j) >> 4][threadIdx.x & 15] = nv[j];
+        if (threadIdx.x < TT) al[threadIdx.x] = expf(nd * a);
+        __syncthreads();
+        if (t0 + TT < end) fetch(t0 + TT);
+        // Four tokens at a time: their vectors are fetched and their read-outs summed over the parts together (rows behind the tile's end are
+        // tokens of step 0 that write nothing).
+#pragma unroll 1
+        for (int t0i = 0; t0i < m; t0i += 4) {
+            float y[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int t = t0i + u;
+                const float x = vs[t][cc], d = al[t];
+                float y0 = 0.f, y1 = 0.f;
+#pragma unroll
+                for (int r = 0; r < R; r += 4) {
+                    const float4 kk = *reinterpret_cast<const float4 *>(&ks[t][(r >> 2) * 32 + part * 4]);
+                    const float4 qq = *reinterpret_cast<const float4 *>(&qs[t][(r >> 2) * 32 + part * 4]);
+                    s[r] = fmaf(kk.x, x, d * s[r]);
+                    s[r + 1] = fmaf(kk.y, x, d * s[r + 1]);
+                    s[r + 2] = fmaf(kk.z, x, d * s[r + 2]);
+                    s[r + 3] = fmaf(kk.w, x, d * s[r + 3]);
+                    y0 = fmaf(qq.x, s[r], y0);
+                    y1 = fmaf(qq.y, s[r + 1], y1);
+                    y0 = fmaf(qq.z, s[r + 2], y0);
+                    y1 = fmaf(qq.w, s[r + 3], y1);
+                }
+                y[u] = y0 + y1;
             }
-            float y = y0 + y1;
-#pragma unroll
-            for (int o = 4; o < 32; o <<= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
-            if (part == 0 && col < p.P) out[(size_t)(t0 + t) * p.H * p.P] = from_f32<OUT>(fmaf(skip, x, y));
+            // lane bits 4 and 3 choose the token, bit 2 is summed over
+            const bool b4 = lane & 16, b3 = lane & 8;
+            const float z0 = (b4 ? y[2] : y[0]) + __shfl_xor_sync(0xffffffffu, b4 ? y[0] : y[2], 16);
+            const float z1 = (b4 ? y[3] : y[1]) + __shfl_xor_sync(0xffffffffu, b4 ? y[1] : y[3], 16);
+            float z = (b3 ? z1 : z0) + __shfl_xor_sync(0xffffffffu, b3 ? z0 : z1, 8);
+            z += __shfl_xor_sync(0xffffffffu, z, 4);
+            const int t = t0i + (b4 ? 2 : 0) + (b3 ? 1 : 0);
+            if (!(lane & 4) && t < m && col < p.P) out[(size_t)(t0 + t) * p.H * p.P] = from_f32<OUT>(fmaf(skip, vs[t][cc], z));
         }
     }
     if (p.final_state)
