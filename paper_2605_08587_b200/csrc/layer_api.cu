@@ -79,6 +79,10 @@ static kla_status conv_args(const kla_desc *d, int32_t channels, int32_t taps, c
 }
 
 // ---- scan -------------------------------------------------------------------------------------------------------------------------
+static bool ssm_widths(const kla_desc *d, int32_t groups)
+{
+    return d->H >= 1 && groups >= 1 && d->H % groups == 0 && d->d_k >= 8 && d->d_k <= 256 && d->d_k % 8 == 0 && d->d_v >= 8 && d->d_v <= 256 && d->d_v % 8 == 0;
+}
 static kla_status ssm_args(const kla_desc *d, int32_t groups, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
                            int64_t v_stride, const float *dt, const float *a, const float *d_skip, SsmParams *p)
 {
@@ -86,8 +90,7 @@ static kla_status ssm_args(const kla_desc *d, int32_t groups, const void *q, int
     CHECK(check_rows(d, &rows));
     if (d->out_dtype != KLA_F32 && d->out_dtype != KLA_BF16) return KLA_ERR_DTYPE;
     if (((!q || !k || !v || !dt) && rows) || !a) return KLA_ERR_NULL;
-    if (d->H < 1 || groups < 1 || d->H % groups) return KLA_ERR_SHAPE;
-    if (d->d_k < 8 || d->d_k > 256 || d->d_k % 8 || d->d_v < 8 || d->d_v > 256 || d->d_v % 8) return KLA_ERR_SHAPE;
+    if (!ssm_widths(d, groups)) return KLA_ERR_SHAPE;
     if (q_stride < (int64_t)groups * d->d_k || k_stride < (int64_t)groups * d->d_k || v_stride < (int64_t)d->H * d->d_v) return KLA_ERR_SHAPE;
     if ((int64_t)(d->n_seq > d->B ? d->n_seq : d->B) * d->H * 16 >= (int64_t)1 << 31) return KLA_ERR_SHAPE;
     const int64_t unit = d->io_dtype == KLA_BF16 ? 8 : 4;   // elements of 16 bytes
@@ -236,7 +239,7 @@ static bool on_tensor_cores(const kla_desc *d, const SsmParams &p)
 size_t kla_ssm_fwd_workspace_bytes(const kla_desc *desc, int32_t groups)
 {
     int64_t rows = 0;
-    if (check_rows(desc, &rows) != KLA_OK || check_sequences(desc) != KLA_OK || desc->H < 1 || groups < 1) return 0;
+    if (check_rows(desc, &rows) != KLA_OK || check_sequences(desc) != KLA_OK || !ssm_widths(desc, groups)) return 0;
     const SsmParams p = ssm_sizes(desc, rows, groups);
     return on_tensor_cores(desc, p) ? ssm_chunk_workspace_bytes(p) : 0;
 }
@@ -275,8 +278,7 @@ kla_status kla_ssm_step(const kla_desc *desc, int32_t groups, const void *q, int
 size_t kla_ssm_bwd_workspace_bytes(const kla_desc *desc, int32_t groups)
 {
     int64_t rows = 0;
-    if (check_rows(desc, &rows) != KLA_OK || check_sequences(desc) != KLA_OK) return 0;
-    if (desc->H < 1 || groups < 1 || desc->H % groups || desc->d_k < 8 || desc->d_k > 256 || desc->d_v < 8 || desc->d_v > 256) return 0;
+    if (check_rows(desc, &rows) != KLA_OK || check_sequences(desc) != KLA_OK || !ssm_widths(desc, groups)) return 0;
     const SsmParams p = ssm_sizes(desc, rows, groups);
     return on_tensor_cores(desc, p) ? ssm_bwd_chunk_workspace_bytes(p) : ssm_bwd_workspace_bytes((int)rows, desc->n_seq, desc->H, groups, desc->d_k, desc->d_v);
 }

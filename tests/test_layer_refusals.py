@@ -159,3 +159,10 @@ def test_arguments_of_another_kind(what, change, error):
     f = {"_conv": kla.kla_conv_fwd, "_ssm": kla.kla_ssm_fwd, "_norm": kla.kla_norm_fwd}[what]
     with pytest.raises(error):
         f(**dict(globals()[what](), **change))
+
+
+@pytest.mark.parametrize("change, groups", [(dict(d_v=0), 2), (dict(d_v=-64), 2), (dict(d_k=0), 2), (dict(d_v=512), 2), (dict(d_k=68), 2), (dict(H=0), 2), (dict(), 3), (dict(), 0),
+                                            (dict(B=0, n_seq=0), 2), (dict(T=-1), 2)])
+def test_scratch_of_calls_that_are_refused(lib, change, groups):
+    assert lib.kla_ssm_fwd_workspace_bytes(ctypes.byref(desc(**change)), groups) == 0
+    assert lib.kla_ssm_bwd_workspace_bytes(ctypes.byref(desc(**change)), groups) == 0
