@@ -41,43 +41,43 @@ __device__ __forceinline__ void window_row(Pack<IO, VEC> &x, const ConvParams &p
                              : nullptr);
 }
 
-// Units of work: (run of tokens, VEC channels), then, where a final state is wanted, (sequence, VEC channels).
-template <typename IO, int W, int VEC, bool SILU>
-__global__ void __launch_bounds__(256) conv_fwd_kernel(ConvParams p, Sequences seqs, int run, int n_runs)
+// The last W - 1 rows of sequence n's window, whatever its length.  (final_state may be init_state: row i is written after row i + len is read.)
+template <typename IO, int W, int VEC>
+__device__ __forceinline__ void last_rows(const ConvParams &p, const Sequences &seqs, int n, int c)
 {
-    const int nvec = p.C / VEC;
-    const long long unit = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int c = (int)(unit % nvec) * VEC;
-    const long long job = unit / nvec;
-    if (job >= n_runs) {   // final states: the last W - 1 rows of the window, whatever a sequence's length
-        const long long n = job - n_runs;
-        if (!p.final_state || n >= p.n_seq) return;
-        const int start = seqs.start((int)n), len = seqs.start((int)n + 1) - start;
-        Pack<IO, VEC> x;
+    const int start = seqs.start(n), len = seqs.start(n + 1) - start;
+    Pack<IO, VEC> x;
 #pragma unroll
-        for (int i = 0; i < W - 1; ++i) {
-            window_row<IO, VEC>(x, p, (int)n, start, len - (W - 1) + i, c);
-            x.store(static_cast<IO *>(p.final_state) + ((size_t)n * (W - 1) + i) * p.C + c);
-        }
+    for (int i = 0; i < W - 1; ++i) {
+        window_row<IO, VEC>(x, p, n, start, len - (W - 1) + i, c);
+        x.store(static_cast<IO *>(p.final_state) + ((size_t)n * (W - 1) + i) * p.C + c);
+    }
+}
+
+// Any number of channels, any stride: a thread to a channel.  Units of work: (run of tokens, channel), then, where a final state is wanted,
+// (sequence, channel).
+template <typename IO, int W, bool SILU>
+__global__ void __launch_bounds__(256) conv_fwd1_kernel(ConvParams p, Sequences seqs, int run, int n_runs)
+{
+    const long long unit = (long long)blockIdx.x * 256 + threadIdx.x, job = unit / p.C;
+    const int c = (int)(unit % p.C);
+    if (job >= n_runs) {
+        if (p.final_state && job - n_runs < p.n_seq) last_rows<IO, W, 1>(p, seqs, (int)(job - n_runs), c);
         return;
     }
     const int r0 = (int)job * run, r1 = min(p.rows, r0 + run);
-    float w[W][VEC], b[VEC];
+    float w[W];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        b[e] = p.bias ? p.bias[c + e] : 0.f;
-#pragma unroll
-        for (int i = 0; i < W; ++i) w[i][e] = p.weight[(size_t)(c + e) * W + i];
-    }
+    for (int i = 0; i < W; ++i) w[i] = p.weight[(size_t)c * W + i];
+    const float b = p.bias ? p.bias[c] : 0.f;
     int seq = seqs.of_row(r0), start = seqs.start(seq), end = seqs.start(seq + 1);
-    float win[W - 1][VEC];
+    float win[W - 1];
     auto fill = [&](int pos) {   // the window before token `pos`
 #pragma unroll
         for (int i = 0; i < W - 1; ++i) {
-            Pack<IO, VEC> x;
-            window_row<IO, VEC>(x, p, seq, start, pos - (W - 1) + i, c);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) win[i][e] = x.get(e);
+            Pack<IO, 1> x;
+            window_row<IO, 1>(x, p, seq, start, pos - (W - 1) + i, c);
+            win[i] = x.get(0);
         }
     };
     fill(r0 - start);
@@ -85,10 +85,10 @@ __global__ void __launch_bounds__(256) conv_fwd_kernel(ConvParams p, Sequences s
     IO *yp = static_cast<IO *>(p.out) + c;
     constexpr int AHEAD = 8;   // rows in flight
     for (int r = r0; r < r1; r += AHEAD) {
-        Pack<IO, VEC> raw[AHEAD];
+        float raw[AHEAD];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j)
-            if (r + j < r1) raw[j].load(xp + (size_t)(r + j) * p.x_stride);
+            if (r + j < r1) raw[j] = to_f32(xp[(size_t)(r + j) * p.x_stride]);
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
             if (r + j >= r1) break;
@@ -100,22 +100,14 @@ __global__ void __launch_bounds__(256) conv_fwd_kernel(ConvParams p, Sequences s
                 } while (end == start && seq + 1 < p.n_seq);
                 fill(0);
             }
-            float y[VEC];
+            float s = b;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float x = raw[j].get(e);
-                float s = b[e];
+            for (int i = 0; i < W - 1; ++i) s = fmaf(w[i], win[i], s);
+            s = fmaf(w[W - 1], raw[j], s);
+            yp[(size_t)(r + j) * p.C] = from_f32<IO>(SILU ? s * sigmoid(s) : s);
 #pragma unroll
-                for (int i = 0; i < W - 1; ++i) s = fmaf(w[i][e], win[i][e], s);
-                s = fmaf(w[W - 1][e], x, s);
-                y[e] = SILU ? s * sigmoid(s) : s;
-#pragma unroll
-                for (int i = 0; i + 1 < W - 1; ++i) win[i][e] = win[i + 1][e];
-                win[W - 2][e] = x;
-            }
-            Pack<IO, VEC> o;
-            o.set(y);
-            o.store(yp + (size_t)(r + j) * p.C);
+            for (int i = 0; i + 1 < W - 1; ++i) win[i] = win[i + 1];
+            win[W - 2] = raw[j];
         }
     }
 }
@@ -128,16 +120,8 @@ __global__ void __launch_bounds__(256, 3) conv_fwd4_kernel(ConvParams p, Sequenc
     const long long unit = (long long)blockIdx.x * 256 + threadIdx.x;
     const int c = (int)(unit % nvec) * 4;
     const long long job = unit / nvec;
-    if (job >= n_runs) {   // final states: the last W - 1 rows of the window, whatever a sequence's length
-        const long long n = job - n_runs;
-        if (!p.final_state || n >= p.n_seq) return;
-        const int start = seqs.start((int)n), len = seqs.start((int)n + 1) - start;
-        Pack<IO, 4> x;
-#pragma unroll
-        for (int i = 0; i < W - 1; ++i) {
-            window_row<IO, 4>(x, p, (int)n, start, len - (W - 1) + i, c);
-            x.store(static_cast<IO *>(p.final_state) + ((size_t)n * (W - 1) + i) * p.C + c);
-        }
+    if (job >= n_runs) {
+        if (p.final_state && job - n_runs < p.n_seq) last_rows<IO, W, 4>(p, seqs, (int)(job - n_runs), c);
         return;
     }
     const int r0 = (int)job * run, r1 = min(p.rows, r0 + run);
@@ -250,69 +234,56 @@ __global__ void __launch_bounds__(128) conv_step_kernel(ConvParams p)
     for (int i = 0; i < W - 1; ++i) x[i + 1].store(state + (size_t)i * p.C);
 }
 
-// A block: 32 x VEC channels and the rows [y rows_per, ..), an eighth of them to each of its warps.  The sums over rows stay in registers,
-// then the warps' are added in shared memory and leave as one partial of [W + 1][C] per block row; conv_reduce_kernel adds those in order.
-template <typename IO, int W, int VEC, bool SILU>
-__global__ void __launch_bounds__(256) conv_bwd_kernel(ConvParams p, Sequences seqs, int rows_per)
+// Any number of channels, any stride: a thread to a channel.  A block: 32 channels and the rows [y rows_per, ..), an eighth of them to each of its
+// warps.  The sums over rows stay in registers, then the warps' are added in shared memory and leave as one partial of [W + 1][C] per block row;
+// conv_reduce_kernel adds those in order.
+template <typename IO, int W, bool SILU>
+__global__ void __launch_bounds__(256) conv_bwd1_kernel(ConvParams p, Sequences seqs, int rows_per)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int c = (blockIdx.x * 32 + lane) * VEC;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     const int b0 = blockIdx.y * rows_per, b1 = min(p.rows, b0 + rows_per);
     const int sub = (rows_per + 7) / 8;
     const int r0 = min(b1, b0 + warp * sub), r1 = min(b1, r0 + sub);
-    float dw[W][VEC], db[VEC];
+    float dw[W], db = 0.f;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        db[e] = 0.f;
-#pragma unroll
-        for (int i = 0; i < W; ++i) dw[i][e] = 0.f;
-    }
+    for (int i = 0; i < W; ++i) dw[i] = 0.f;
     if (r0 < r1 && c < p.C) {
-        float w[W][VEC], b[VEC];
+        float w[W];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            b[e] = p.bias ? p.bias[c + e] : 0.f;
-#pragma unroll
-            for (int i = 0; i < W; ++i) w[i][e] = p.weight[(size_t)(c + e) * W + i];
-        }
+        for (int i = 0; i < W; ++i) w[i] = p.weight[(size_t)c * W + i];
+        const float b = p.bias ? p.bias[c] : 0.f;
         int seq = seqs.of_row(r0), start = seqs.start(seq), end = seqs.start(seq + 1);
-        float win[W - 1][VEC], acc[W][VEC];   // acc[s]: gradient of row t - s so far
+        float win[W - 1], acc[W];   // acc[s]: gradient of row t - s so far
         auto fill = [&](int pos) {
 #pragma unroll
             for (int i = 0; i < W - 1; ++i) {
-                Pack<IO, VEC> x;
-                window_row<IO, VEC>(x, p, seq, start, pos - (W - 1) + i, c);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) win[i][e] = x.get(e);
+                Pack<IO, 1> x;
+                window_row<IO, 1>(x, p, seq, start, pos - (W - 1) + i, c);
+                win[i] = x.get(0);
             }
         };
         fill(r0 - start);
 #pragma unroll
-        for (int s = 0; s < W; ++s)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) acc[s][e] = 0.f;
+        for (int s = 0; s < W; ++s) acc[s] = 0.f;
         const IO *xp = static_cast<const IO *>(p.x) + c, *gp = static_cast<const IO *>(p.d_out) + c, *fp = static_cast<const IO *>(p.d_final);
         IO *dxp = static_cast<IO *>(p.dx) + c;
         const int last = r1 + W - 1;   // the rows behind the run whose windows reach into it
         constexpr int AHEAD = 4;
         for (int t0 = r0; t0 < last; t0 += AHEAD) {
-            Pack<IO, VEC> xr[AHEAD], gr[AHEAD];
+            float xr[AHEAD], gr[AHEAD];
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j)
                 if (t0 + j < last && t0 + j < p.rows) {
-                    xr[j].load(xp + (size_t)(t0 + j) * p.x_stride);
-                    gr[j].load(gp + (size_t)(t0 + j) * p.C);
+                    xr[j] = to_f32(xp[(size_t)(t0 + j) * p.x_stride]);
+                    gr[j] = to_f32(gp[(size_t)(t0 + j) * p.C]);
                 }
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 const int t = t0 + j;
                 if (t >= last) break;
 #pragma unroll
-                for (int s = W - 1; s > 0; --s)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) acc[s][e] = acc[s - 1][e];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) acc[0][e] = 0.f;
+                for (int s = W - 1; s > 0; --s) acc[s] = acc[s - 1];
+                acc[0] = 0.f;
                 if (t < p.rows) {
                     if (t == end) {
                         do {
@@ -322,69 +293,50 @@ __global__ void __launch_bounds__(256) conv_bwd_kernel(ConvParams p, Sequences s
                         } while (end == start && seq + 1 < p.n_seq);
                         fill(0);
                     }
-                    if (fp && t >= end - (W - 1)) {
-                        Pack<IO, VEC> f;
-                        f.load(fp + ((size_t)seq * (W - 1) + (t - (end - (W - 1)))) * p.C + c);
+                    if (fp && t >= end - (W - 1)) acc[0] = to_f32(fp[((size_t)seq * (W - 1) + (t - (end - (W - 1)))) * p.C + c]);
+                    float g = gr[j];
+                    if (SILU) {
+                        float s = b;
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) acc[0][e] = f.get(e);
+                        for (int i = 0; i < W - 1; ++i) s = fmaf(w[i], win[i], s);
+                        s = fmaf(w[W - 1], xr[j], s);
+                        const float sig = sigmoid(s);
+                        g *= sig * fmaf(s, 1.f - sig, 1.f);
                     }
-                    const int pos = t - start;
-                    const bool mine = t < r1;
+                    if (t < r1) {
+                        db += g;
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float x = xr[j].get(e);
-                        float g = gr[j].get(e);
-                        if (SILU) {
-                            float s = b[e];
-#pragma unroll
-                            for (int i = 0; i < W - 1; ++i) s = fmaf(w[i][e], win[i][e], s);
-                            s = fmaf(w[W - 1][e], x, s);
-                            const float sig = sigmoid(s);
-                            g *= sig * fmaf(s, 1.f - sig, 1.f);
-                        }
-                        if (mine) {
-                            db[e] += g;
-#pragma unroll
-                            for (int i = 0; i < W - 1; ++i) dw[i][e] = fmaf(g, win[i][e], dw[i][e]);
-                            dw[W - 1][e] = fmaf(g, x, dw[W - 1][e]);
-                        }
-#pragma unroll
-                        for (int s = 0; s < W; ++s)
-                            if (s <= pos) acc[s][e] = fmaf(w[W - 1 - s][e], g, acc[s][e]);
-#pragma unroll
-                        for (int i = 0; i + 1 < W - 1; ++i) win[i][e] = win[i + 1][e];
-                        win[W - 2][e] = x;
+                        for (int i = 0; i < W - 1; ++i) dw[i] = fmaf(g, win[i], dw[i]);
+                        dw[W - 1] = fmaf(g, xr[j], dw[W - 1]);
                     }
+#pragma unroll
+                    for (int s = 0; s < W; ++s)
+                        if (s <= t - start) acc[s] = fmaf(w[W - 1 - s], g, acc[s]);
+#pragma unroll
+                    for (int i = 0; i + 1 < W - 1; ++i) win[i] = win[i + 1];
+                    win[W - 2] = xr[j];
                 }
                 const int done = t - (W - 1);   // (below r1: t is below r1 + W - 1)
-                if (done >= r0) {
-                    Pack<IO, VEC> o;
-                    o.set(acc[W - 1]);
-                    o.store(dxp + (size_t)done * p.C);
-                }
+                if (done >= r0) dxp[(size_t)done * p.C] = from_f32<IO>(acc[W - 1]);
             }
         }
     }
-    __shared__ float sums[8][32 * VEC];
+    __shared__ float sums[8][32];
 #pragma unroll
     for (int i = 0; i <= W; ++i) {
         __syncthreads();
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) sums[warp][lane * VEC + e] = i < W ? dw[i < W ? i : 0][e] : db[e];
+        sums[warp][lane] = i < W ? dw[i < W ? i : 0] : db;
         __syncthreads();
-        for (int x = threadIdx.x; x < 32 * VEC; x += 256) {
-            const int ch = blockIdx.x * 32 * VEC + x;
-            if (ch < p.C) {
-                float s = 0.f;
+        if (warp == 0 && c < p.C) {
+            float s = 0.f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) s += sums[k][x];
-                p.partial[((size_t)blockIdx.y * (W + 1) + i) * p.C + ch] = s;
-            }
+            for (int k = 0; k < 8; ++k) s += sums[k][lane];
+            p.partial[((size_t)blockIdx.y * (W + 1) + i) * p.C + c] = s;
         }
     }
 }
 
-// Four channels to a thread, in pairs; otherwise as conv_bwd_kernel.
+// Four channels to a thread, in pairs; otherwise as conv_bwd1_kernel.
 template <typename IO, int W, bool SILU>
 __global__ void __launch_bounds__(256, 2) conv_bwd4_kernel(ConvParams p, Sequences seqs, int rows_per)
 {
@@ -602,8 +554,12 @@ static cudaError_t with_taps(int taps, bool silu, F f)
 }
 
 template <typename IO, int VEC>
-static cudaError_t conv_fwd_v(const ConvParams &p, cudaStream_t stream)
+static cudaError_t conv_fwd_v(const ConvParams &all, cudaStream_t stream)
 {
+    ConvParams p = all;
+    // A state updated in place is written once the runs, which read it, are done.
+    const bool in_place = p.final_state && p.final_state == p.init_state && p.rows > 0;
+    if (in_place) p.final_state = nullptr;
     const Sequences seqs = {p.cu_seqlens, p.T, p.n_seq};
     const int nvec = p.C / VEC;
     // Runs as long as give every SM its three blocks once (a second wave would be a short one), no shorter than 8 rows: the rows before a run
@@ -613,12 +569,16 @@ static cudaError_t conv_fwd_v(const ConvParams &p, cudaStream_t stream)
     const int n_runs = ceil_div(p.rows, run);
     const long long units = ((long long)n_runs + (p.final_state ? p.n_seq : 0)) * nvec;
     if (units == 0) return cudaSuccess;
-    return with_taps(p.taps, p.silu, [&](auto W, auto SILU) {
+    const cudaError_t err = with_taps(p.taps, p.silu, [&](auto W, auto SILU) {
         if constexpr (VEC == 4) conv_fwd4_kernel<IO, W(), SILU()><<<ceil_div(units, 256), 256, 0, stream>>>(p, seqs, (int)run, n_runs);
-        else conv_fwd_kernel<IO, W(), VEC, SILU()><<<ceil_div(units, 256), 256, 0, stream>>>(p, seqs, (int)run, n_runs);
+        else conv_fwd1_kernel<IO, W(), SILU()><<<ceil_div(units, 256), 256, 0, stream>>>(p, seqs, (int)run, n_runs);
         count_launch(1);
         return cudaGetLastError();
     });
+    if (err != cudaSuccess || !in_place) return err;
+    p.final_state = all.final_state;
+    p.rows = 0;   // (the states alone)
+    return conv_fwd_v<IO, VEC>(p, stream);
 }
 
 template <typename IO, int VEC>
@@ -659,7 +619,7 @@ static cudaError_t conv_bwd_v(const ConvParams &p, cudaStream_t stream)
     return with_taps(p.taps, p.silu, [&](auto W, auto SILU) {
         const dim3 grid((unsigned)ceil_div(p.C, 32 * VEC), (unsigned)ny);
         if constexpr (VEC == 4) conv_bwd4_kernel<IO, W(), SILU()><<<grid, 256, 0, stream>>>(p, seqs, per);
-        else conv_bwd_kernel<IO, W(), VEC, SILU()><<<grid, 256, 0, stream>>>(p, seqs, per);
+        else conv_bwd1_kernel<IO, W(), SILU()><<<grid, 256, 0, stream>>>(p, seqs, per);
         conv_reduce_kernel<<<ceil_div((long long)(W() + 1) * p.C, 32), 512, 0, stream>>>(p.partial, ny, W(), p.C, p.dweight, p.dbias);
         count_launch(2);
         if (p.dinit) {

@@ -484,7 +484,7 @@ PyObject *dict(std::initializer_list<std::pair<const char *, at::Tensor>> items)
     }
     return r;
 }
-// Runs `call` without the interpreter's lock and raises for a status other than KLA_OK.
+// Runs `call` without the interpreter's lock, so that it must not raise, and raises for a status other than KLA_OK.
 template <typename F>
 void run(F call)
 {
@@ -519,6 +519,7 @@ struct Conv {
     int64_t C, W, stride = 0;
     void *xa;
     float *wa, *ba;
+    int32_t channels, taps;
     Conv(PyObject *x_, PyObject *w_, PyObject *b_, int dims) : x(tensor(x_, "x")), weight(tensor(w_, "weight")), bias(opt_tensor(b_, "bias"))
     {
         io = io_of(x, "x");
@@ -529,6 +530,8 @@ struct Conv {
         xa = row_addr(x, 1, "x", &stride);
         wa = param(&weight, x, {C, W}, "weight");
         ba = param(bias, x, {C}, "bias");
+        channels = small(C);
+        taps = small(W);
     }
 };
 
@@ -549,7 +552,8 @@ PyObject *conv_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (fg) fin = *fg;
         else if (integer(a[9]) && c.W > 0) fin = at::empty(state, c.x.options());
         void *oa = array(&out, c.x, c.x.sizes(), c.io, "out"), *fa = fin.defined() ? array(&fin, c.x, state, c.io, "final_state") : nullptr;
-        run([&] { return kla_conv_fwd(&d, small(c.C), small(c.W), c.xa, c.stride, c.wa, c.ba, ia, oa, fa); });
+        if (oa == c.xa && d.B > 0 && d.T > 0) fail(PyExc_ValueError, "must not be the input", "out");
+        run([&] { return kla_conv_fwd(&d, c.channels, c.taps, c.xa, c.stride, c.wa, c.ba, ia, oa, fa); });
         return pair(out, fin);
     });
 }
@@ -569,7 +573,7 @@ PyObject *conv_step(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (og) out = *og;
         else out = at::empty(c.x.sizes(), c.x.options());
         void *oa = array(&out, c.x, c.x.sizes(), c.io, "out");
-        run([&] { return kla_conv_step(&d, small(c.C), small(c.W), c.xa, c.stride, c.wa, c.ba, sa, oa); });
+        run([&] { return kla_conv_step(&d, c.channels, c.taps, c.xa, c.stride, c.wa, c.ba, sa, oa); });
         return wrap(out);
     });
 }
@@ -591,9 +595,9 @@ PyObject *conv_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
         at::Tensor dx = at::empty(c.x.sizes(), c.x.options()), dw = at::empty({c.C, c.W}, c.weight.options()), db, di;
         if (c.ba) db = at::empty({c.C}, c.weight.options());
         if (integer(a[9]) && c.W > 0) di = at::empty(state, c.x.options());
-        at::Tensor ws = scratch(&d, c.x, kla_conv_bwd_workspace_bytes(&d, small(c.C), small(c.W)));
+        at::Tensor ws = scratch(&d, c.x, kla_conv_bwd_workspace_bytes(&d, c.channels, c.taps));
         run([&] {
-            return kla_conv_bwd(&d, small(c.C), small(c.W), c.xa, c.stride, c.wa, c.ba, ia, ga, fa, dx.data_ptr(), dw.data_ptr<float>(),
+            return kla_conv_bwd(&d, c.channels, c.taps, c.xa, c.stride, c.wa, c.ba, ia, ga, fa, dx.data_ptr(), dw.data_ptr<float>(),
                                 db.defined() ? db.data_ptr<float>() : nullptr, di.defined() ? di.data_ptr() : nullptr);
         });
         return dict({{"dx", dx}, {"dweight", dw}, {"dbias", db}, {"dinit_state", di}});
@@ -608,6 +612,7 @@ struct Ssm {
     int64_t H, G, N, P, qs = 0, ks = 0, vs = 0;
     void *qa, *ka, *va;
     float *dta, *aa, *sa;
+    int32_t groups;
     std::vector<int64_t> state;   // shape, but for its first entry
     Ssm(PyObject *const *x, PyObject *skip_, int lead)
         : q(tensor(x[0], "q")), k(tensor(x[1], "k")), v(tensor(x[2], "v")), dt(tensor(x[3], "dt")), a(tensor(x[4], "a")), skip(opt_tensor(skip_, "d_skip"))
@@ -631,6 +636,7 @@ struct Ssm {
         aa = param(&a, v, {H}, "a");
         sa = param(skip, v, {H}, "d_skip");
         state = {0, H, N, P};
+        groups = small(G);
     }
     void into(kla_desc *d)
     {
@@ -661,8 +667,8 @@ PyObject *ssm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
         void *oa = array(&out, s.v, s.v.sizes(), io_of(out, "out"), "out"), *fa = fin.defined() ? array(&fin, s.v, s.state, at::kFloat, "final_state") : nullptr;
         d.out_dtype = dtype_code(out.scalar_type());
         d.status_word = status_word(a[14], s.v.device());
-        at::Tensor ws = scratch(&d, s.v, kla_ssm_fwd_workspace_bytes(&d, small(s.G)));
-        run([&] { return kla_ssm_fwd(&d, small(s.G), s.qa, s.qs, s.ka, s.ks, s.va, s.vs, s.dta, s.aa, s.sa, static_cast<float *>(ia), oa, static_cast<float *>(fa)); });
+        at::Tensor ws = scratch(&d, s.v, kla_ssm_fwd_workspace_bytes(&d, s.groups));
+        run([&] { return kla_ssm_fwd(&d, s.groups, s.qa, s.qs, s.ka, s.ks, s.va, s.vs, s.dta, s.aa, s.sa, static_cast<float *>(ia), oa, static_cast<float *>(fa)); });
         return pair(out, fin);
     });
 }
@@ -684,7 +690,7 @@ PyObject *ssm_step(PyObject *, PyObject *const *a, Py_ssize_t n)
         else out = at::empty(s.v.sizes(), s.v.options().dtype(dtype_arg(a[8], s.v)));
         void *oa = array(&out, s.v, s.v.sizes(), io_of(out, "out"), "out");
         d.out_dtype = dtype_code(out.scalar_type());
-        run([&] { return kla_ssm_step(&d, small(s.G), s.qa, s.qs, s.ka, s.ks, s.va, s.vs, s.dta, s.aa, s.sa, static_cast<float *>(sa), oa); });
+        run([&] { return kla_ssm_step(&d, s.groups, s.qa, s.qs, s.ka, s.ks, s.va, s.vs, s.dta, s.aa, s.sa, static_cast<float *>(sa), oa); });
         return wrap(out);
     });
 }
@@ -709,9 +715,9 @@ PyObject *ssm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
         at::Tensor ddt = at::empty(s.dt.sizes(), f32), da = at::empty({s.H}, f32), dd, di;
         if (s.sa) dd = at::empty({s.H}, f32);
         if (integer(a[12])) di = at::empty(s.state, f32);
-        at::Tensor ws = scratch(&d, s.v, kla_ssm_bwd_workspace_bytes(&d, small(s.G)));
+        at::Tensor ws = scratch(&d, s.v, kla_ssm_bwd_workspace_bytes(&d, s.groups));
         run([&] {
-            return kla_ssm_bwd(&d, small(s.G), s.qa, s.qs, s.ka, s.ks, s.va, s.vs, s.dta, s.aa, s.sa, static_cast<float *>(ia), ga, static_cast<float *>(fa),
+            return kla_ssm_bwd(&d, s.groups, s.qa, s.qs, s.ka, s.ks, s.va, s.vs, s.dta, s.aa, s.sa, static_cast<float *>(ia), ga, static_cast<float *>(fa),
                                dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ddt.data_ptr<float>(), da.data_ptr<float>(),
                                dd.defined() ? dd.data_ptr<float>() : nullptr, di.defined() ? di.data_ptr<float>() : nullptr);
         });
@@ -727,6 +733,7 @@ struct Norm {
     int64_t D, group, xs = 0, zs = 0;
     void *xa, *ra, *za = nullptr;
     float *wa, *sa, eps;
+    int32_t width, per;   // channels of a row, of a group
     Norm(PyObject *x_, PyObject *w_, PyObject *eps_, PyObject *r_, PyObject *s_, PyObject *z_, PyObject *group_)
         : x(tensor(x_, "x")), weight(tensor(w_, "weight")), residual(opt_tensor(r_, "residual")), scale(opt_tensor(s_, "scale")), gate(opt_tensor(z_, "gate"))
     {
@@ -746,6 +753,8 @@ struct Norm {
             za = row_addr(*gate, 1, "gate", &zs);
             same_device(*gate, x, "gate");
         }
+        width = small(D);
+        per = small(group);
     }
     kla_desc desc(PyObject *flags) const
     {
@@ -771,7 +780,7 @@ PyObject *norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
         else if (m.residual) res = at::empty(m.x.sizes(), m.residual->options());
         if (rg && !m.residual) fail(PyExc_ValueError, "needs a residual", "residual_out");
         void *oa = array(&out, m.x, m.x.sizes(), m.io, "out"), *ra = res.defined() ? array(&res, m.x, m.x.sizes(), m.res, "residual_out") : nullptr;
-        run([&] { return kla_norm_fwd(&d, small(m.D), small(m.group), m.xa, m.xs, m.ra, dtype_code(m.res), m.sa, m.za, m.zs, m.wa, m.eps, oa, ra); });
+        run([&] { return kla_norm_fwd(&d, m.width, m.per, m.xa, m.xs, m.ra, dtype_code(m.res), m.sa, m.za, m.zs, m.wa, m.eps, oa, ra); });
         return pair(out, res);
     });
 }
@@ -790,9 +799,9 @@ PyObject *norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (m.residual) dr = at::empty(m.x.sizes(), m.residual->options());
         if (m.scale) ds = at::empty({m.D}, m.weight.options());
         if (m.gate) dz = at::empty(m.x.sizes(), m.x.options());
-        at::Tensor ws = scratch(&d, m.x, kla_norm_bwd_workspace_bytes(&d, small(m.D), small(m.group)));
+        at::Tensor ws = scratch(&d, m.x, kla_norm_bwd_workspace_bytes(&d, m.width, m.per));
         run([&] {
-            return kla_norm_bwd(&d, small(m.D), small(m.group), m.xa, m.xs, m.ra, dtype_code(m.res), m.sa, m.za, m.zs, m.wa, m.eps, ga, da, dx.data_ptr(),
+            return kla_norm_bwd(&d, m.width, m.per, m.xa, m.xs, m.ra, dtype_code(m.res), m.sa, m.za, m.zs, m.wa, m.eps, ga, da, dx.data_ptr(),
                                 dr.defined() ? dr.data_ptr() : nullptr, ds.defined() ? ds.data_ptr<float>() : nullptr,
                                 dz.defined() ? dz.data_ptr() : nullptr, dw.data_ptr<float>());
         });

@@ -134,3 +134,18 @@ def test_gradient_against_differences():
         up[i], down[i] = (args[i] + h * u).contiguous(), (args[i] - h * u).contiguous()
         diff = (loss(*up) - loss(*down)) / (2 * h)
         assert abs(diff - float((g[name] * u).sum())) <= 2e-3 * max(1.0, float(g[name].norm())), name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("C, dtype", [(64, torch.bfloat16), (9, torch.bfloat16), (20, torch.float32)])
+@pytest.mark.parametrize("lens", [[300], [40, 0, 1, 2, 90], [0, 0], [1]])
+def test_states_in_place(lens, C, dtype):
+    """final_state may be init_state: the same bits as apart.  The output may not be the input."""
+    x, w, b, s, _, _, seqs = _case(lens, C, 4, dtype)
+    y, fin = kla_conv_fwd(x, w, bias=b, init_state=s, **seqs)
+    state = s.clone()
+    y2, fin2 = kla_conv_fwd(x, w, bias=b, init_state=state, final_state=state, **seqs)
+    assert fin2.data_ptr() == state.data_ptr() and torch.equal(y, y2) and torch.equal(state, fin)
+    if sum(lens):
+        with pytest.raises(ValueError, match="out"):
+            kla_conv_fwd(x, w, bias=b, out=x, **seqs)

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from layer_refs import check, grads, leaf, norm
-from paper_2605_08587_b200 import KLA_FLAG_GATE_FIRST, KLA_FLAG_NONE, kla_norm_bwd, kla_norm_fwd
+from paper_2605_08587_b200 import KLA_FLAG_GATE_FIRST, KLA_FLAG_NONE, KlaError, kla_norm_bwd, kla_norm_fwd
 
 DEV = "cuda:0"
 EPS = 1e-6
@@ -133,3 +133,13 @@ def test_sums_over_rows_do_not_vary():
     for _ in range(3):
         again = kla_norm_bwd(x, w, EPS, dy, d_residual_out=dr, **a)
         assert all(torch.equal(first[n], again[n]) for n in ("dx", "dweight", "dresidual", "dscale"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("group, error", [(-1, ValueError), (1 << 40, ValueError), (0, KlaError), (7, KlaError)])
+def test_groups_that_are_refused(group, error):
+    x, w = torch.ones(4, 64, dtype=BF, device=DEV), torch.ones(64, device=DEV)
+    with pytest.raises(error):
+        kla_norm_fwd(x, w, 1e-6, group=group)
+    with pytest.raises(error):
+        kla_norm_bwd(x, w, 1e-6, x, group=group)
