@@ -227,7 +227,8 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
             earlier += __shfl_xor_sync(0xffffffffu, earlier, o);
         }
         const float before = __shfl_up_sync(0xffffffffu, prefix, 1);
-        const float F = suffix + later + (lane ? before : 0.f) + earlier + whole * all;
+        // (a decay that is zero has no gradient, where the sums leave the rounding of what cancels in them)
+        const float F = dt * a * LOG2E < NO_DECAY ? 0.f : suffix + later + (lane ? before : 0.f) + earlier + whole * all;
         if (in) p.a.ddt[row_out * p.a.H + h] = fmaf(a, F, acc[0][2][t] + acc[1][2][t]);
         float da = in ? dt * F : 0.f;
 #pragma unroll

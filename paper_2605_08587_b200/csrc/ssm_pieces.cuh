@@ -163,6 +163,9 @@ constexpr int STATE_ELEMS = 128 * NS;
 // however far the block's start lies back.
 //   a2 inclusive sum inside the block
 //   r = 2^a2 (from the block's start);  cf = dt 2^(sum of what follows in the block)
+// A token's log2 decay below NO_DECAY counts as that (its power of two is zero in fp32 all the same): a token that wipes the state would otherwise leave
+// sums whose differences have lost the digits of the tokens behind it.
+constexpr float NO_DECAY = -152.f;
 struct alignas(16) Scalars {
     float a2[C], r[C], cf[C], dt[C];
 };
@@ -171,7 +174,7 @@ struct BlockScan {
     __device__ __forceinline__ BlockScan(float dt, float a)
     {
         const int lane = threadIdx.x & 31;
-        const float x = dt * a * LOG2E;
+        const float l = dt * a * LOG2E, x = l < NO_DECAY ? NO_DECAY : l;   // (NaN stays)
         float up = x, down = x;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -186,7 +189,6 @@ struct BlockScan {
     }
 };
 
-// Tensor map of a bf16 [rows][cols] array, rows `stride` elements apart, boxes of 128 rows x 64 elements, 128-byte swizzle.
 // State passes (ssm_state.cu).  The states that the parts of a sequence start from: forward the state before the part, in reverse the gradient
 // of the state behind it.
 cudaError_t launch_part_starts(const SsmParams &a, const Parts &parts, bool reverse, cudaStream_t stream);
@@ -194,6 +196,7 @@ cudaError_t launch_part_starts(const SsmParams &a, const Parts &parts, bool reve
 // state to a.dinit.
 cudaError_t launch_chunk_states(const SsmParams &a, const Parts &parts, bool reverse, float *states, cudaStream_t stream);
 
+// Tensor map of a bf16 [rows][cols] array, rows `stride` elements apart, boxes of 128 rows x 64 elements, 128-byte swizzle.
 bool make_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint64_t stride);
 
 }  // namespace ssm

@@ -447,7 +447,8 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
                 if (lane + o < 32) suffix += t;
                 if (lane >= o) before += u;
             }
-            const float f = suffix + (before - z) + expf((float)l[QB - 1]) * sg;
+            // (a decay of zero, below 2^-150, has no gradient, where the sums leave the rounding of what cancels in them)
+            const float f = d * a < -104.f ? 0.f : suffix + (before - z) + expf((float)l[QB - 1]) * sg;
             if (lane < m) p.ddt[(size_t)(start + lane) * p.H + h] = fmaf(a, f, direct);
             float da = lane < m ? d * f : 0.f;
             for (int o = 16; o > 0; o >>= 1) da += __shfl_xor_sync(0xffffffffu, da, o);

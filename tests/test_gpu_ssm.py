@@ -269,3 +269,40 @@ def test_a_wait_that_runs_out_is_reported(N, P):
     y, _ = kla_ssm_fwd(*args, **seqs)
     y1, _ = kla_ssm_fwd(*args, flags=KLA_FLAG_FORCE_SIMT, **seqs)
     assert float((y.double() - y1.double()).norm() / y1.double().norm()) <= 2.0 ** -8
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("flags", [KLA_FLAG_NONE, KLA_FLAG_FORCE_SIMT])
+@pytest.mark.parametrize("N, P", [(64, 64), (128, 64)])
+def test_tokens_that_wipe_the_state(N, P, flags):
+    """Steps of 1e6 and decays of exp(-1e6 and less) among ordinary ones, at most one to 32 tokens: what follows them keeps its digits (the sums of
+    log decays that count stay below those of the other tests), and the gradient of a decay that is zero is zero."""
+    lens, H, G = [200, 90], 2, 1
+    s, seqs, dy, df = make(lens, H, G, N, P, BF, seed=3)
+    at = [5, 40, 64, 127, 128, 199, 200, 250]
+    s["dt"][0, at] = 1e6
+    y, fin = kla_ssm_fwd(**s, **seqs, out_dtype=F32, flags=flags)
+    g = kla_ssm_bwd(s["q"], s["k"], s["v"], s["dt"], s["a"], dy, d_skip=s["d_skip"], init_state=s["init_state"], d_final_state=df, flags=flags, **seqs)
+    torch.cuda.synchronize()
+    leaves, (ry, rf), sizes, (my, mf) = reference(s, lens)
+    rel = rel_of(lens, N, P)
+    check(y[0], ry, my, rel, "out")
+    check(fin, rf, mf, 2.0 ** -17 + (max(lens) + 64) * 2.0 ** -24, "final_state")
+    r = grads((ry, rf), (dy[0], df), leaves)
+    m = grads((my, mf), (dy[0].abs(), df.abs()), sizes)
+    for i, n in enumerate(("dq", "dk", "dv")):
+        check(g[n][0], r[i], m[i], 2 * rel + 2.0 ** -8, n)
+    check(g["dd"], r[5], m[5], 2 * rel, "dd")
+    check(g["dinit_state"], r[6], m[6], 2 * rel, "dinit_state")
+    check(g["ddt"][0, at], r[3][at], m[3][at], 2 * rel, "ddt")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens, H, N, P", [([70, 0, 200], 2, 64, 64), ([2000], 1, 128, 64), ([33, 0, 5], 2, 24, 16)])
+def test_states_in_place(lens, H, N, P):
+    """final_state may be init_state: the same bits as apart, in one pass, in parts and on CUDA cores."""
+    s, seqs, _, _ = make(lens, H, 1, N, P, BF, seed=1)
+    y, fin = kla_ssm_fwd(**s, **seqs)
+    state = s["init_state"].clone()
+    y2, fin2 = kla_ssm_fwd(**dict(s, init_state=state), final_state=state, **seqs)
+    assert fin2.data_ptr() == state.data_ptr() and torch.equal(y, y2) and torch.equal(state, fin)
