@@ -24,6 +24,11 @@
 // Decays are products of exponentials of sums that do not exceed zero (for a < 0): inside a block of 32 tokens one exponential per
 // element, between blocks the product of a factor per row, one per pair of blocks and one per column, which costs two multiplications.
 //
+// What bounds it: the port of the shared memory.  Of the 4 900 cycles of a chunk at N = 128 the products' operands take 2 050, the loads' tiles 640, and the
+// roles' own reads and writes 2 300 (counted).  P of the next chunk formed before the outputs of the last, with P and q S there twice and k once,
+// 209 us for 201 on 8 x 4096 tokens of 32 heads (k comes too late); what helped last were accesses: one arrival per warp at a barrier and outputs staged without
+// bank conflicts (201 -> 196).
+//
 // Few long sequences are cut into parts that run side by side: a first pass forms what each part adds to a state of zero and its whole
 // decay, ssm_parts_kernel chains them, and the main pass starts every part from its true state.  The decay is a scalar per
 // head, so that the chain needs no products (the delta rule's segments need whole transition maps).
@@ -137,13 +142,13 @@ __device__ void decay_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
         const float w = cf * exp2f(warp == 0 ? t1 + t2 + t3 : warp == 1 ? t2 + t3 : warp == 2 ? t3 : 0.f);
         if (c > 0 && !bar_wait(&sm.bar[B_WX1], c - 1, &sm.abort_flag)) break;   // the last chunk's weights have been used
         sm.weight[t] = w;
-        mbar_arrive(&sm.bar[B_W]);
+        warp_arrive(&sm.bar[B_W]);
         if (c > 0 && !bar_wait(&sm.bar[B_P], c - 1, &sm.abort_flag)) break;     // and its scalars
         sm.sc.a2[t] = b.a2;
         sm.sc.r[t] = r;
         sm.sc.cf[t] = cf;
         sm.sc.dt[t] = dt;
-        mbar_arrive(&sm.bar[B_SCAL]);
+        warp_arrive(&sm.bar[B_SCAL]);
         dt = next_dt;
     }
 }
@@ -174,7 +179,7 @@ __device__ void state_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
             }
         fence_async_smem();
         tc_fence_before();
-        mbar_arrive(&sm.bar[B_S]);
+        warp_arrive(&sm.bar[B_S]);
     };
     write_parts();
     float gamma = 0.f;
@@ -184,7 +189,7 @@ __device__ void state_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
         tc_fence_after();
         join(S, tm, gamma);
         tc_fence_before();
-        mbar_arrive(&sm.bar[B_JOIN]);
+        warp_arrive(&sm.bar[B_JOIN]);
         return true;
     };
     bool ok = true;
@@ -200,14 +205,14 @@ __device__ void state_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
                 for (int b2 = 0; b2 < N / 64; ++b2) zero_half_row(sm.k[st][b2], t, half);
             }
             fence_async_smem();
-            mbar_arrive(&sm.bar[B_CLEAN]);
+            warp_arrive(&sm.bar[B_CLEAN]);
             ok = ok && bar_wait(&sm.bar[B_CLEAN], 0, &sm.abort_flag);
         }
         if (ok && c > 0) ok = bar_wait(&sm.bar[B_DS0 + (c - 1) % STAGES], (c - 1) / STAGES, &sm.abort_flag);
         if (!ok) break;
         weigh(sm.x[st], sm.w, 0, sm.weight);
         fence_async_smem();
-        mbar_arrive(&sm.bar[B_WX0]);
+        warp_arrive(&sm.bar[B_WX0]);
         const float *tot = sm.tot[c & 1];
         const float next_gamma = exp2f(tot[0] + tot[1] + tot[2] + tot[3]);
         if (c > 0) {
@@ -218,7 +223,7 @@ __device__ void state_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
         gamma = next_gamma;
         weigh(sm.x[st], sm.w, 64, sm.weight);
         fence_async_smem();
-        mbar_arrive(&sm.bar[B_WX1]);
+        warp_arrive(&sm.bar[B_WX1]);
     }
     ok = ok && joined(wk.chunks - 1);
     if (wk.fin && row && ok) write_row(S, wk.fin + (size_t)t * p.a.P + half * HS);
@@ -302,7 +307,7 @@ __device__ void output_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
         for (int i = 0; i < 4; ++i) x[i] = *piece(sm.x[st], t, 4 * half + i);
         fence_async_smem();
         tc_fence_before();
-        mbar_arrive(&sm.bar[B_P]);
+        warp_arrive(&sm.bar[B_P]);
         return true;
     };
     // o of chunk c
@@ -312,6 +317,7 @@ __device__ void output_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
         tc_fence_after();
         unsigned char *stage = sm.p[0][half];   // (read by the product that has just completed, and written by this warp alone)
         constexpr int PC = std::is_same<OUT, float>::value ? 8 : 4;   // 16-byte pieces of a row
+        const int swap = PC == 4 ? 4 * (lane & 1) : 0;   // (odd rows in the other half of their line: two rows are read at a time)
         const float2 e2 = f2(e);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
@@ -325,7 +331,7 @@ __device__ void output_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
             tmem_ld16(tm + TM_Y2<PARTS> + half * 32 + g * 16, y2);
             if (g == 1) {
                 tc_fence_before();
-                mbar_arrive(&sm.bar[B_YFREE]);
+                warp_arrive(&sm.bar[B_YFREE]);
             }
             float2 y[8];
 #pragma unroll
@@ -341,20 +347,20 @@ __device__ void output_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
             } else {
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                    *piece(stage, t, 2 * g + i) = make_uint4(pack2(y[4 * i]), pack2(y[4 * i + 1]), pack2(y[4 * i + 2]), pack2(y[4 * i + 3]));
+                    *piece(stage, t, swap ^ (2 * g + i)) = make_uint4(pack2(y[4 * i]), pack2(y[4 * i + 1]), pack2(y[4 * i + 2]), pack2(y[4 * i + 3]));
             }
         }
         // through shared memory, so that a store is 16 bytes of one token and a warp's stores are whole sectors
         __syncwarp();
-        const int rr = warp * 32 + lane / PC;
+        const int rr = warp * 32 + lane / PC, from = PC == 4 ? (lane & 3) ^ (lane & 4) : lane % PC;
         OUT *to = out + (size_t)(c * C + rr) * stride + lane % PC * (16 / sizeof(OUT));
         if (m == C) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 32 / PC) *reinterpret_cast<uint4 *>(to + i * stride) = *piece(stage, rr + i, lane % PC);
+            for (int i = 0; i < 32; i += 32 / PC) *reinterpret_cast<uint4 *>(to + i * stride) = *piece(stage, rr + i, from);
         } else {
 #pragma unroll 1
             for (int i = 0; i < 32; i += 32 / PC)
-                if (rr + i < m) *reinterpret_cast<uint4 *>(to + i * stride) = *piece(stage, rr + i, lane % PC);
+                if (rr + i < m) *reinterpret_cast<uint4 *>(to + i * stride) = *piece(stage, rr + i, from);
         }
         __syncwarp();
         return true;
@@ -498,7 +504,7 @@ ssm_chunk_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__
         return;
     }
     if (tid == 0) {
-        for (int b = 0; b < B_COUNT; ++b) mbar_init(&sm.bar[b], b == B_TOT ? 4 : b == B_W || b == B_SCAL ? DECAY_T : b >= B_CLEAN && b < B_CB ? 256 : 1);
+        for (int b = 0; b < B_COUNT; ++b) mbar_init(&sm.bar[b], b == B_TOT || b == B_W || b == B_SCAL ? 4 : b >= B_CLEAN && b < B_CB ? 8 : 1);
         sm.abort_flag = 0;
         mbar_fence_init();
         tma_prefetch_desc(&tq);

@@ -38,6 +38,13 @@ __device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatil
     return __all_sync(0xffffffffu, ok);
 }
 
+// One arrival for the whole warp (a barrier takes those of 32 lanes one after another), of what all its lanes have done before.
+__device__ __forceinline__ void warp_arrive(uint64_t *bar)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+}
+
 // Asks for a box of a tensor map to be brought into L2.
 __device__ __forceinline__ void prefetch_2d(const void *tmap, int x, int y)
 {

@@ -103,7 +103,7 @@ __device__ void work(Smem &sm, const Params &p, const Piece &pc, int h, int sl, 
         weigh(sm.x, sm.w, w);
         fence_async_smem();
         tc_fence_before();
-        mbar_arrive(&sm.bar[B_WX]);
+        warp_arrive(&sm.bar[B_WX]);
         if (!(ok = bar_wait(&sm.bar[B_DS], cx, &sm.abort_flag))) break;
         tc_fence_after();
         join(S, tm, gamma);
@@ -144,7 +144,7 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__
         return;
     }
     if (tid == 0) {
-        for (int b = 0; b < B_COUNT; ++b) mbar_init(&sm.bar[b], b == B_TOT ? 8 : b == B_WX ? 256 : 1);
+        for (int b = 0; b < B_COUNT; ++b) mbar_init(&sm.bar[b], b == B_TOT || b == B_WX ? 8 : 1);
         sm.abort_flag = 0;
         mbar_fence_init();
         tma_prefetch_desc(&tk);
