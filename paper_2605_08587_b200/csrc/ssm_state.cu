@@ -5,8 +5,8 @@
 //     reverse   G' = e^{l_Q} G + sum_i q_i (e^{l_i} do_i)^T                  from the last to the first: G behind a chunk -> G before it
 //
 // the same kernel with other tiles, weights and order.  One product per chunk, k^T [w v in three bf16 parts]; the state stays in registers, in
-// fp32.  A chunk is one chain (decays, weights, product, state), so two blocks share an SM and fill each other's gaps: 96 KB of tiles each,
-// single-buffered, 256 columns of tensor memory.
+// fp32.  A chunk is one chain (decays, weights, product, state), so two blocks share an SM and fill each other's gaps: 112 KB of tiles each,
+// 256 columns of tensor memory.
 #include "ssm_pieces.cuh"
 
 namespace kla {
@@ -16,11 +16,11 @@ namespace {
 
 constexpr int NT = 256 + 32;   // 256 work, one warp issues and loads
 
-enum Bar { B_TILES = 0, B_TOT, B_W, B_CLEAN, B_WX, B_DS, B_COUNT };
+enum Bar { B_K = 0, B_X /* of even and odd chunks */, B_TOT = B_X + 2, B_WX, B_DS, B_COUNT };
 
 struct Smem {
     alignas(1024) unsigned char k[2][TILE];   // k (reverse: q): [64 of N][token][64]
-    alignas(1024) unsigned char x[TILE];      // v (reverse: do): [token][64 columns]
+    alignas(1024) unsigned char x[2][TILE];   // v (reverse: do) of chunks in turn: [token][64 columns]
     alignas(1024) unsigned char w[3][TILE];   // parts of the weighted v
     float tot[2][4];
     alignas(8) uint64_t bar[B_COUNT];
@@ -68,45 +68,53 @@ __device__ void work(Smem &sm, const Params &p, const Piece &pc, int h, int sl, 
     const Slots slots(p.a.cu_seqlens, p.a.T);
     float *out = p.states ? p.states + (((slots.first(pc.n) + pc.g * (p.parts.seg_len / C)) * p.a.H + h) * (p.a.P / NS) + sl) * STATE_ELEMS + threadIdx.x * 4 : nullptr;
     const size_t out_step = (size_t)p.a.H * (p.a.P / NS) * STATE_ELEMS;
-    bool ok = true;
-#pragma unroll 1
-    for (int cx = 0; cx < chunks; ++cx) {
-        const int c = REV ? chunks - 1 - cx : cx, m = min(C, pc.len - c * C);
+    // This token's weight in the cx-th chunk, and the chunk's decay
+    auto decays = [&](int cx, float &w, float &gamma) {
         const BlockScan b(dt, a);
-        float *tot = sm.tot[cx & 1];
+        float *tot = sm.tot[cx & 1];   // (of two chunks before: read before the last one's product)
         if (lane == 0) {
             if (half == 0) tot[warp] = b.tot;
             mbar_arrive(&sm.bar[B_TOT]);
         }
-        float w = REV ? exp2f(b.a2) : dt * exp2f(b.rest);
+        w = token(cx) < pc.len ? (REV ? exp2f(b.a2) : dt * exp2f(b.rest)) : 0.f;
         if (cx + 1 < chunks) dt = token(cx + 1) < pc.len ? dtp[(size_t)token(cx + 1) * p.a.H] : 0.f;
-        if (out) {   // the state before this chunk (in order), a layout of whole cache lines: piece, thread, four columns
-#pragma unroll
-            for (int i = 0; i < HS / 4; ++i) store4(out + c * out_step + i * 1024, make_float4(S[2 * i].x, S[2 * i].y, S[2 * i + 1].x, S[2 * i + 1].y));
-        }
-        if (!(ok = bar_wait(&sm.bar[B_TOT], cx, &sm.abort_flag))) break;
+        if (!bar_wait(&sm.bar[B_TOT], cx, &sm.abort_flag)) return false;
         const float t0 = tot[0], t1 = tot[1], t2 = tot[2], t3 = tot[3];
-        const float other = REV ? (warp == 0 ? 0.f : warp == 1 ? t0 : warp == 2 ? t0 + t1 : t0 + t1 + t2)
-                                : (warp == 0 ? t1 + t2 + t3 : warp == 1 ? t2 + t3 : warp == 2 ? t3 : 0.f);
-        w *= exp2f(other);
-        if (t >= m) w = 0.f;
-        const float gamma = exp2f(t0 + t1 + t2 + t3);
+        w *= exp2f(REV ? (warp == 0 ? 0.f : warp == 1 ? t0 : warp == 2 ? t0 + t1 : t0 + t1 + t2)
+                       : (warp == 0 ? t1 + t2 + t3 : warp == 1 ? t2 + t3 : warp == 2 ? t3 : 0.f));
+        gamma = exp2f(t0 + t1 + t2 + t3);
         total += t0 + t1 + t2 + t3;
-        if (!(ok = bar_wait(&sm.bar[B_TILES], cx, &sm.abort_flag))) break;
+        return true;
+    };
+    float w = 0.f, gamma = 0.f, next_gamma = 0.f;
+    bool ok = decays(0, w, gamma);
+#pragma unroll 1
+    for (int cx = 0; ok && cx < chunks; ++cx) {
+        const int c = REV ? chunks - 1 - cx : cx, m = min(C, pc.len - c * C);
+        if (!(ok = bar_wait(&sm.bar[B_X + (cx & 1)], cx >> 1, &sm.abort_flag))) break;
         if (m < C) {   // rows behind the sequence's end: another sequence's, perhaps not finite; nothing of them may meet a zero weight
+            if (!(ok = bar_wait(&sm.bar[B_K], cx, &sm.abort_flag))) break;
             if (t >= m) {
-                zero_half_row(sm.x, t, half);
+                zero_half_row(sm.x[cx & 1], t, half);
 #pragma unroll
                 for (int b2 = 0; b2 < N / 64; ++b2) zero_half_row(sm.k[b2], t, half);
             }
         }
-        weigh(sm.x, sm.w, w);
+        weigh(sm.x[cx & 1], sm.w, w);
         fence_async_smem();
         tc_fence_before();
         warp_arrive(&sm.bar[B_WX]);
+        // While the product runs: the state before this chunk (in order) in a layout of whole cache lines (piece, thread, four columns), and the next
+        // chunk's decays
+        if (out) {
+#pragma unroll
+            for (int i = 0; i < HS / 4; ++i) store4(out + c * out_step + i * 1024, make_float4(S[2 * i].x, S[2 * i].y, S[2 * i + 1].x, S[2 * i + 1].y));
+        }
+        if (cx + 1 < chunks && !(ok = decays(cx + 1, w, next_gamma))) break;
         if (!(ok = bar_wait(&sm.bar[B_DS], cx, &sm.abort_flag))) break;
         tc_fence_after();
         join(S, tm, gamma);
+        gamma = next_gamma;
     }
     tc_fence_before();
     if (!ok || sm.abort_flag) return;
@@ -162,14 +170,19 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__
 #pragma unroll 1
         for (int cx = 0; cx < chunks; ++cx) {
             auto y = [&](int i) { return pc.tok0 + (REV ? chunks - 1 - i : i) * C; };
-            if (tid == 256) {
-                mbar_expect_tx(&sm.bar[B_TILES], (NB + 1) * TILE);
-                for (int b = 0; b < NB; ++b) tma_load_2d(sm.k[b], &tk, xk + b * 64, y(cx), &sm.bar[B_TILES]);
-                tma_load_2d(sm.x, &tv, xv, y(cx), &sm.bar[B_TILES]);
-                if (cx + 1 < chunks) {   // the next chunk's on their way to L2 meanwhile
+            if (tid == 256) {   // k is there for one chunk, v a chunk ahead; more on their way to L2 meanwhile
+                auto values = [&](int i) {
+                    mbar_expect_tx(&sm.bar[B_X + (i & 1)], TILE);
+                    tma_load_2d(sm.x[i & 1], &tv, xv, y(i), &sm.bar[B_X + (i & 1)]);
+                };
+                if (cx == 0) values(0);
+                mbar_expect_tx(&sm.bar[B_K], NB * TILE);
+                for (int b = 0; b < NB; ++b) tma_load_2d(sm.k[b], &tk, xk + b * 64, y(cx), &sm.bar[B_K]);
+                if (cx + 1 < chunks) {
+                    values(cx + 1);
                     for (int b = 0; b < NB; ++b) prefetch_2d(&tk, xk + b * 64, y(cx + 1));
-                    prefetch_2d(&tv, xv, y(cx + 1));
                 }
+                if (cx + 2 < chunks) prefetch_2d(&tv, xv, y(cx + 2));
             }
             __syncwarp();
             if (cx + 2 < chunks)
@@ -177,7 +190,7 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__
                     const int tok = y(cx + 2) + i;
                     if (tok < pc.tok0 + pc.len) prefetch_line(p.a.dt + (size_t)tok * p.a.H + h);
                 }
-            if (!bar_wait(&sm.bar[B_TILES], cx, &sm.abort_flag) || !bar_wait(&sm.bar[B_WX], cx, &sm.abort_flag)) break;
+            if (!bar_wait(&sm.bar[B_K], cx, &sm.abort_flag) || !bar_wait(&sm.bar[B_WX], cx, &sm.abort_flag)) break;
             tc_fence_after();
 #pragma unroll
             for (int b = 0; b < 2; ++b) mma4_bf16_lo<128, 128>(sm.tmem, k_mn + b * 512, w_mn + b * 512, idesc_bf16(128, 192, 1, 1), b);
