@@ -14,6 +14,8 @@
  * kla_chunk_fwd evaluates it for whole sequences with the chunkwise-parallel solver
  * (Algorithm 1, right panel; Eqs. 7-9); kla_decode_step applies it to one new token per
  * sequence with the state updated in place.  The result does not depend on the chunk length.
+ * The operators that a layer has around such a mixer, and the selective state space scan, which is another one, are in the last
+ * section of this file.
  *
  * General rules
  *  - Every data pointer is a DEVICE pointer unless stated otherwise; every buffer is owned by the
@@ -21,7 +23,7 @@
  *    process-wide bookkeeping that no result depends on: the launch counter read by kla_launch_count, the
  *    driver entry point used to encode tensor maps, and, for kla_chunk_fwd_static_scratch, the device address
  *    of its built-in scratch array (looked up once per device; stale after cudaDeviceReset).
- *  - All arrays are dense, row-major, last index contiguous, 16-byte aligned.
+ *  - All arrays are dense, row-major, last index contiguous, 16-byte aligned, but for those whose call says otherwise.
  *  - Work is enqueued on desc->stream and the call returns without synchronising.  Argument
  *    errors are detected on the host before anything is launched and reported through the
  *    return value; nothing is launched in that case.
@@ -61,14 +63,14 @@ typedef enum { KLA_F32 = 0, KLA_BF16 = 1 } kla_dtype;
 /* desc->flags */
 #define KLA_FLAG_NONE 0
 /* Force the fp32 kernel on CUDA cores (a scan over blocks of four tokens) even where the tensor-core kernel applies (used to
- * cross-check the two device paths against each other and against the oracle). */
+ * cross-check the two device paths against each other and against the oracle).  kla_ssm_fwd and kla_ssm_bwd: their kernels on CUDA cores. */
 #define KLA_FLAG_FORCE_SIMT 1
 /* Layer-edge variants named by the paper; both default to off (the recurrence at the top of this file). */
 #define KLA_FLAG_COEFF_ETA 4              /* beta_t = eta_t: the gated-delta-rule baseline coefficient of Section 2,
                                              without the key-norm division of Eq. 3 (eps is then unused)          */
 #define KLA_FLAG_QNORM 8                  /* o_t = S_t^T q_t / ||q_t||: the read-out as Algorithm 1 (left) prints it */
 /* Not part of the supported flag set: used by the library's own tests of the error path.  The tensor-core kernels (kla_chunk_fwd,
- * kla_chunk_span_map, and kla_bwd with bf16 inputs) withhold one internal completion signal, so that a bounded device-side wait
+ * kla_chunk_span_map, and kla_bwd, kla_ssm_fwd and kla_ssm_bwd with bf16 inputs) withhold one internal completion signal, so that a bounded device-side wait
  * runs out (about one second), every CTA gives up in an orderly way and KLA_ERR_TIMEOUT appears in *status_word.  Outputs are
  * then undefined; the context stays usable. */
 #define KLA_INTERNAL_FLAG_TEST_TIMEOUT 16
@@ -99,7 +101,7 @@ typedef enum { KLA_F32 = 0, KLA_BF16 = 1 } kla_dtype;
  * KLA_FLAG_SEGMENTS(g) asks for it (the longest sequence in g pieces, every sequence in pieces of that length), the long
  * sequences are cut into pieces that start from warm-up runs; if the decay does not allow that, the plain launch runs
  * instead (again decided on the device).  The workspace then also holds the piece tables. */
-#define KLA_FLAG_NO_SEGMENTS 2            /* never cut sequences into segments                              */
+#define KLA_FLAG_NO_SEGMENTS 2            /* never cut sequences into segments (kla_ssm_fwd, kla_ssm_bwd: into parts) */
 #define KLA_FLAG_EXACT_SEGMENTS 128       /* segments always from chained transition maps, never from warm-up runs */
 #define KLA_FLAG_SEGMENTS(g) ((g) << 8)   /* force g segments per sequence, 2 <= g <= 255 (fewer if T is short) */
 /* Operators around a mixer (below). */
@@ -121,13 +123,15 @@ typedef struct {
     int32_t io_dtype;   /* kla_dtype of q, k, v                                                 */
     int32_t out_dtype;  /* kla_dtype of out                                                     */
     int32_t flags;      /* KLA_FLAG_*                                                           */
-    void *workspace;           /* DEVICE scratch of at least kla_chunk_fwd_workspace_bytes()    */
+    void *workspace;           /* DEVICE scratch of at least kla_chunk_fwd_workspace_bytes(), or
+                                  what the call's own query says                                */
     size_t workspace_bytes;
     int32_t *status_word;      /* optional DEVICE int32, zeroed by the caller; a kernel whose
                                   bounded wait expires stores KLA_ERR_TIMEOUT there and exits, one
                                   that finds its shared memory misplaced KLA_ERR_ALIGN
-                                  (kla_chunk_fwd and its variants, kla_chunk_span_map, kla_bwd): the
-                                  call has then returned KLA_OK, and its outputs are undefined */
+                                  (kla_chunk_fwd and its variants, kla_chunk_span_map, kla_bwd,
+                                  kla_ssm_fwd, kla_ssm_bwd): the call has then returned KLA_OK, and its
+                                  outputs are undefined                                         */
     void *stream;              /* cudaStream_t (NULL = default stream)                          */
 } kla_desc;
 
@@ -315,7 +319,7 @@ kla_status kla_bwd(const kla_desc *desc, const void *q, const void *k, const voi
  * ---- Operators around a mixer ------------------------------------------------------------------------------------
  *
  * What a layer puts before, beside and behind the mixers above.  Sequences, dtypes, workspace, status word and stream are those of
- * kla_desc; each call names its own channel counts.  "Rows" are tokens: row b T + t, or the packed tokens.  Inputs whose call takes a
+ * kla_desc; each call names its own channel counts.  "Rows" are tokens: row b T + t, or the packed tokens; fewer than 2^31 - 2^21.  Inputs whose call takes a
  * stride may be slices of wider arrays: consecutive rows `stride` elements apart, the elements of a row dense; everything else
  * is dense.  Pointers 16-byte aligned, those of weight, bias, scale, dt, a and d_skip 4-byte.  Outputs must not overlap inputs except where said.  Sums, states and norms are fp32.
  *
@@ -326,7 +330,7 @@ kla_status kla_bwd(const kla_desc *desc, const void *q, const void *k, const voi
  * (KLA_FLAG_CONV_LINEAR: y_t = p_t).  Inputs before a sequence's first token are rows of its state, oldest first, or zeros.
  *   desc: B, T, n_seq, cu_seqlens, host_seqlens, io_dtype, flags, stream are used
  *   x [rows, channels] io_dtype; 2 <= taps <= 4; weight [channels, taps], bias [channels] (or NULL) fp32
- *   init_state, final_state [n_seq, taps - 1, channels] io_dtype, or NULL; an input is stored as it is
+ *   init_state, final_state [n_seq, taps - 1, channels] io_dtype, or NULL; an input is stored as it is; final_state may be init_state
  *   out [rows, channels] io_dtype
  * kla_conv_step: one token per sequence (desc->T 1, no cu_seqlens); x, out [B, channels]; the state moves on by one row in place.
  * kla_conv_bwd: d_out, dx [rows, channels] io_dtype; d_final_state, dinit_state as the states, or NULL; dweight [channels, taps], dbias
@@ -351,7 +355,15 @@ kla_status kla_conv_bwd(const kla_desc *desc, int32_t channels, int32_t taps, co
  *   desc: B, T, H, d_k, d_v (multiples of 8 up to 256), n_seq, cu_seqlens, host_seqlens, io_dtype, out_dtype, flags, workspace,
  *     status_word and stream are used
  *   q, k [rows, groups, d_k], v [rows, H, d_v] io_dtype, row strides multiples of 16 bytes;  dt [rows, H], a [H], d_skip [H] (or NULL) fp32
- *   init_state, final_state [n_seq, H, d_k, d_v] fp32 or NULL; out [rows, H, d_v] out_dtype
+ *   init_state, final_state [n_seq, H, d_k, d_v] fp32 or NULL (final_state may be init_state); out [rows, H, d_v] out_dtype
+ * dt a must be finite; a decay below 2^-150 is zero.  bf16 inputs with d_k 64 or 128 and d_v a multiple of 64 run in chunks of 128 tokens
+ * (counted from a sequence's start) on the tensor cores, everything else token by token in fp32; in chunks an input that is not finite
+ * may spoil outputs of its sequence from the chunk's start on, not only those behind it.  Of bf16 outputs each term carries one rounding
+ * to bf16 before the sum is rounded to it, of fp32 outputs one to 16 bits; states and the gradients of dt, a, d_skip and init_state are
+ * fp32 throughout.
+ * Few long sequences are cut into parts that run side by side (KLA_FLAG_NO_SEGMENTS: not), which the workspace of
+ * kla_ssm_fwd_workspace_bytes is for; kla_ssm_bwd_workspace_bytes: the states and their gradients at every chunk, about
+ * 8 d_v bytes per row and head, on CUDA cores d_k d_v / 4.
  * kla_ssm_step: one token per sequence (desc->T 1, no cu_seqlens), the state updated in place.
  * kla_ssm_bwd: d_out [rows, H, d_v] io_dtype; d_final_state, dinit_state as the states or NULL; dq, dk [rows, groups, d_k], dv [rows, H,
  *   d_v] io_dtype, dense; ddt [rows, H], da [H], dd [H] (or NULL) fp32.  The states are recomputed.

@@ -391,7 +391,8 @@ def kla_dg_decode_step(q, k, v, log_alpha, eta, eps, state_inout, out=None, out_
 def kla_conv_fwd(x, weight, bias=None, init_state=None, out=None, final_state=None, cu_seqlens=None, host_seqlens=None, flags=KLA_FLAG_NONE,
                  want_final_state=True):
     """Short causal depthwise convolution with SiLU (include/kla.h: kla_conv_fwd).  x [B, T, C] fp32 or bf16; weight [C, taps], 2 to 4 taps, and
-    bias [C] fp32; init_state, final_state [n_seq, taps - 1, C] in x's dtype: the inputs before the first and up to the last token.
+    bias [C] fp32; init_state, final_state [n_seq, taps - 1, C] in x's dtype: the inputs before the first and up to the last token (one
+    tensor may be both).
     Packed input as kla_chunk_fwd.  KLA_FLAG_CONV_LINEAR: no SiLU.  Returns (out, final_state)."""
     if _host is None:
         load()
@@ -423,7 +424,7 @@ def kla_ssm_fwd(q, k, v, dt, a, d_skip=None, init_state=None, out=None, final_st
                 flags=KLA_FLAG_NONE, want_final_state=True, status_word=None):
     """Selective state space scan (include/kla.h: kla_ssm_fwd): S_t = exp(dt_t a) S + dt_t k_t v_t^T, o_t = S_t^T q_t + d_skip v_t.
     q, k [B, T, G, d_k], v [B, T, H, d_v] fp32 or bf16, each group's q and k serving H / G heads; dt [B, T, H], a [H], d_skip [H] fp32;
-    states [n_seq, H, d_k, d_v] fp32.  Packed input, out_dtype and `status_word` as kla_chunk_fwd.  Returns (out, final_state)."""
+    states [n_seq, H, d_k, d_v] fp32, one tensor for both if wanted.  Packed input, out_dtype and `status_word` as kla_chunk_fwd.  Returns (out, final_state)."""
     if _host is None:
         load()
     if cu_seqlens is not None and host_seqlens is None:

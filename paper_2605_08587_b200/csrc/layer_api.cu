@@ -28,7 +28,7 @@ static kla_status check_rows(const kla_desc *d, int64_t *rows)
     if (d->B < 1 || d->T < 0) return KLA_ERR_SHAPE;
     if (d->status_word && (reinterpret_cast<uintptr_t>(d->status_word) & 3u)) return KLA_ERR_ALIGN;
     *rows = (int64_t)d->B * d->T;
-    return *rows < (int64_t)1 << 31 ? KLA_OK : KLA_ERR_SHAPE;
+    return *rows < ((int64_t)1 << 31) - (1 << 21) ? KLA_OK : KLA_ERR_SHAPE;   // (room for the strides of loops over rows)
 }
 static kla_status check_sequences(const kla_desc *d)
 {

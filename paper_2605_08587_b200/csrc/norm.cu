@@ -6,7 +6,8 @@
 // Backward, with g the gradient of u r:  du = r (g - u r c),  c = mean(g o u r);  dw = sum over rows of (dy o act) o u r.  Both sums a row
 // needs, of u^2 and of g o u, are known before r is, so they are formed together.
 //
-// Memory-bound: every array passes once.  A thread owns eight neighbouring channels (16 bytes of bf16) of every row its block
+// Memory-bound: every array passes once.  8 x 4096 rows, bf16, residual fp32, width 1024: 69 us, 5.8 TB/s; gated backward, width 2048 in groups of 128: 139 us, 4.8 TB/s
+// (bound by registers: with two rows requested ahead 137 us, but spills for the longest rows; three blocks of 256 threads per SM 152 us).  A thread owns eight neighbouring channels (16 bytes of bf16) of every row its block
 // takes, so weights are loaded once and the sums over rows (dw, dscale) stay in its registers; the next row's operands are
 // requested before the current row's sums are exchanged.  Groups of up to 32 threads exchange by shuffles; longer ones also
 // through shared memory, behind one barrier (two buffers in turn).  The norm is of the sum in fp32, before u is rounded to the residual's type.

@@ -6,7 +6,8 @@
 //
 // the same kernel with other tiles, weights and order.  One product per chunk, k^T [w v in three bf16 parts]; the state stays in registers, in
 // fp32.  A chunk is one chain (decays, weights, product, state), so two blocks share an SM and fill each other's gaps: 112 KB of tiles each,
-// 256 columns of tensor memory.
+// 256 columns of tensor memory.  v comes a chunk ahead and the next decays are formed while the product runs; k, needed last, is there once.  A pass over
+// 8 x 4096 tokens of 32 heads (N = 128) that writes every chunk's state, 268 MB: about 105 us.
 #include "ssm_pieces.cuh"
 
 namespace kla {

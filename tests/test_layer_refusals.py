@@ -166,3 +166,9 @@ def test_arguments_of_another_kind(what, change, error):
 def test_scratch_of_calls_that_are_refused(lib, change, groups):
     assert lib.kla_ssm_fwd_workspace_bytes(ctypes.byref(desc(**change)), groups) == 0
     assert lib.kla_ssm_bwd_workspace_bytes(ctypes.byref(desc(**change)), groups) == 0
+
+
+def test_more_rows_than_loops_can_step_over(lib):
+    for T in ((1 << 31) - (1 << 21), (1 << 31) - 1):
+        d = desc(B=1, n_seq=1, T=T)
+        assert conv(lib, d) == SHAPE and ssm(lib, d) == SHAPE and norm(lib, d) == SHAPE
