@@ -306,3 +306,22 @@ def test_states_in_place(lens, H, N, P):
     state = s["init_state"].clone()
     y2, fin2 = kla_ssm_fwd(**dict(s, init_state=state), final_state=state, **seqs)
     assert fin2.data_ptr() == state.data_ptr() and torch.equal(y, y2) and torch.equal(state, fin)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H, G, N, P", [(4, 2, 64, 64), (6, 2, 128, 64)])
+def test_backward_of_more_chunks_than_blocks_run_at_once(H, G, N, P):
+    """Between one and two chunks (times groups) to an SM: the second round's share their heads among several blocks."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    lens = [1 + 5 * i % 13 for i in range(sms // 2 + 12)] + [0, 300]
+    s, seqs, dy, df = make(lens, H, G, N, P, BF, seed=4)
+    g = kla_ssm_bwd(s["q"], s["k"], s["v"], s["dt"], s["a"], dy, d_skip=s["d_skip"], init_state=s["init_state"], d_final_state=df, **seqs)
+    torch.cuda.synchronize()
+    leaves, outs, sizes, mags = reference(s, lens)
+    r, m = grads(outs, (dy[0], df), leaves), grads(mags, (dy[0].abs(), df.abs()), sizes)
+    a, dt, rel = s["a"].double().cpu(), s["dt"][0].double().cpu(), 2 * rel_of(lens, N, P)
+    for i, n in enumerate(("dq", "dk", "dv")):
+        check(g[n][0], r[i], m[i], rel + 2.0 ** -8, n)
+    check(g["ddt"][0], r[3] + a * r[4], m[3] + a.abs() * m[4], rel, "ddt")
+    check(g["da"], (dt * r[4]).sum(0), (dt * m[4]).sum(0), rel + sum(lens) * 2.0 ** -24, "da")
+    check(g["dinit_state"], r[6], m[6], rel, "dinit_state")
