@@ -45,7 +45,7 @@ template <typename IO, typename OUT, int R>
 __global__ void __launch_bounds__(128) ssm_scan_kernel(SsmParams p, Sequences seqs)
 {
     __shared__ __align__(16) float ks[TT][8 * R], qs[TT][8 * R];
-    __shared__ float vs[TT][16], al[TT];
+    __shared__ float vs[TT][16], xs[TT][16], al[TT];   // xs: dt v
     const int cols = (p.P + 15) / 16;
     const int cb = blockIdx.x % cols, h = blockIdx.x / cols % p.H, n = blockIdx.x / cols / p.H, g = h / (p.H / p.G);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = lane >> 2, cc = warp * 4 + (lane & 3), col = cb * 16 + cc;
@@ -60,23 +60,29 @@ __global__ void __launch_bounds__(128) ssm_scan_kernel(SsmParams p, Sequences se
     const IO *q = static_cast<const IO *>(p.q) + g * p.N, *k = static_cast<const IO *>(p.k) + g * p.N, *v = static_cast<const IO *>(p.v) + h * p.P;
     OUT *out = static_cast<OUT *>(p.out) + h * p.P + col;
     const float a = p.a[h], skip = p.skip ? p.skip[h] : 0.f;
-    // The next tile's operands wait in registers while this one's tokens run.
-    float nq[R], nk[R], nv[2], nd = 0.f;
+    // The next tile's operands wait in registers, as loaded, while this one's tokens run (a conversion or a product would wait for the load).
+    IO nq[R], nk[R], nv[2];
+    float nd = 0.f, ndv[2];
     auto fetch = [&](int t0) {
         const int m = end - t0;
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const int i = threadIdx.x + 128 * j, t = i / (8 * R), x = i % (8 * R);
-            nq[j] = nk[j] = 0.f;
+            nq[j] = nk[j] = from_f32<IO>(0.f);
             if (t < m && x < p.N) {
-                nq[j] = to_f32(q[(size_t)(t0 + t) * p.q_stride + x]);
-                nk[j] = to_f32(k[(size_t)(t0 + t) * p.k_stride + x]) * p.dt[(size_t)(t0 + t) * p.H + h];
+                nq[j] = q[(size_t)(t0 + t) * p.q_stride + x];
+                nk[j] = k[(size_t)(t0 + t) * p.k_stride + x];
             }
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int i = threadIdx.x + 128 * j, t = i >> 4, c = cb * 16 + (i & 15);
-            nv[j] = t < m && c < p.P ? to_f32(v[(size_t)(t0 + t) * p.v_stride + c]) : 0.f;
+            nv[j] = from_f32<IO>(0.f);
+            ndv[j] = 0.f;
+            if (t < m && c < p.P) {
+                nv[j] = v[(size_t)(t0 + t) * p.v_stride + c];
+                ndv[j] = p.dt[(size_t)(t0 + t) * p.H + h];
+            }
         }
         if (threadIdx.x < TT) nd = threadIdx.x < m ? p.dt[(size_t)(t0 + threadIdx.x) * p.H + h] : 0.f;
     };
@@ -87,11 +93,15 @@ __global__ void __launch_bounds__(128) ssm_scan_kernel(SsmParams p, Sequences se
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const int i = threadIdx.x + 128 * j;
-            qs[i / (8 * R)][i % (8 * R)] = nq[j];
-            ks[i / (8 * R)][i % (8 * R)] = nk[j];
+            qs[i / (8 * R)][i % (8 * R)] = to_f32(nq[j]);
+            ks[i / (8 * R)][i % (8 * R)] = to_f32(nk[j]);
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) vs[(threadIdx.x + 128 * j) >> 4][threadIdx.x & 15] = nv[j];
+        for (int j = 0; j < 2; ++j) {
+            const float x = to_f32(nv[j]);
+            vs[(threadIdx.x + 128 * j) >> 4][threadIdx.x & 15] = x;
+            xs[(threadIdx.x + 128 * j) >> 4][threadIdx.x & 15] = ndv[j] * x;
+        }
         if (threadIdx.x < TT) al[threadIdx.x] = expf(nd * a);
         __syncthreads();
         if (t0 + TT < end) fetch(t0 + TT);
@@ -103,7 +113,7 @@ __global__ void __launch_bounds__(128) ssm_scan_kernel(SsmParams p, Sequences se
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int t = t0i + u;
-                const float x = vs[t][cc], d = al[t];
+                const float x = xs[t][cc], d = al[t];
                 float y0 = 0.f, y1 = 0.f;
 #pragma unroll
                 for (int r = 0; r < R; r += 4) {
