@@ -25,20 +25,6 @@ namespace kla {
 // consecutive bytes of a vector in shared memory.
 constexpr int TT = 16;   // tokens staged at a time
 
-template <typename IO>
-struct SsmTile {   // one stage: vectors of TT tokens as fp32
-    template <int R>
-    static __device__ __forceinline__ void load(float (*dst)[8 * R], const IO *src, int64_t stride, int t0, int n_tok, int N, const float *times)
-    {
-        for (int i = threadIdx.x; i < TT * 8 * R; i += blockDim.x) {
-            const int t = i / (8 * R), n = i % (8 * R);
-            float x = 0.f;
-            if (t < n_tok && n < N) x = to_f32(src[(size_t)(t0 + t) * stride + n]);
-            dst[t][n] = times ? x * times[t] : x;
-        }
-    }
-};
-
 // Forward.  A warp: 4 columns of the state x 8 parts of its rows, R rows to a thread; a block: 16 columns.  Bound by the latency of one token after another
 // and of a warp's sums over the parts: 8 packed sequences of up to 1024 tokens, 8 heads, N = P = 64, fp32: 129 us (a token at a time, 176).
 template <typename IO, typename OUT, int R>
@@ -218,6 +204,7 @@ __global__ void __launch_bounds__(128) ssm_step_kernel(SsmParams p)
 // Chunks of QB tokens, counted per sequence from its first token.  Chunk c of sequence n has slot start(n) / QB + n + c: slots of different sequences
 // do not meet, and there are at most rows / QB + n_seq of them.
 constexpr int QB = 32;
+static_assert(QB == 2 * TT, "whole tiles to a chunk");
 
 // The state before every chunk (REV false) or the gradient of the state behind it (REV true: from the last chunk to the first,
 // G <- exp(dt a) (G + q do^T)), at [slot][H][N][P].  Layout of threads as in the forward.
@@ -225,11 +212,11 @@ template <typename IO, int R, bool REV>
 __global__ void __launch_bounds__(128) ssm_states_kernel(SsmParams p, Sequences seqs, float *states)
 {
     __shared__ __align__(16) float ks[TT][8 * R];
-    __shared__ float vs[TT][16], al[TT], dts[TT];
+    __shared__ float xs[TT][16], al[TT];   // xs: dt v (REV: do)
     const int cols = (p.P + 15) / 16;
     const int cb = blockIdx.x % cols, h = blockIdx.x / cols % p.H, n = blockIdx.x / cols / p.H, g = h / (p.H / p.G);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = lane >> 2, cc = warp * 4 + (lane & 3), col = cb * 16 + cc;
-    const int start = seqs.start(n), end = seqs.start(n + 1), chunks = (end - start + QB - 1) / QB;
+    const int start = seqs.start(n), end = seqs.start(n + 1), tiles = (end - start + TT - 1) / TT;
     const size_t unit = ((size_t)n * p.H + h) * p.N * p.P, slot0 = (size_t)(start / QB) + n;
     const float *from = REV ? p.d_final : p.init_state;
     float s[R];
@@ -248,36 +235,52 @@ __global__ void __launch_bounds__(128) ssm_states_kernel(SsmParams p, Sequences 
             if (row < p.N && col < p.P) to[(size_t)row * p.P + col] = s[r];
         }
     };
-    for (int cx = 0; cx < chunks; ++cx) {
-        const int c = REV ? chunks - 1 - cx : cx;
-        put(states + ((slot0 + c) * p.H + h) * p.N * p.P);
-        const int b0 = start + c * QB, b1 = min(end, b0 + QB);
-        for (int tx = 0; tx < QB; tx += TT) {
-            const int t0 = REV ? b0 + QB - TT - tx : b0 + tx, m = min(TT, b1 - t0);
-            if (m <= 0) continue;
-            __syncthreads();
-            if (threadIdx.x < TT) {
-                const float d = threadIdx.x < m ? p.dt[(size_t)(t0 + threadIdx.x) * p.H + h] : 0.f;
-                dts[threadIdx.x] = d;
-                al[threadIdx.x] = expf(d * a);
-            }
-            for (int i = threadIdx.x; i < TT * 16; i += 128) {
-                const int t = i >> 4, cl = cb * 16 + (i & 15);
-                vs[t][i & 15] = t < m && cl < p.P ? to_f32(v[(size_t)(t0 + t) * vs_stride + cl]) : 0.f;
-            }
-            __syncthreads();
-            SsmTile<IO>::template load<R>(ks, k, ks_stride, t0, m, p.N, REV ? nullptr : dts);
-            __syncthreads();
-            for (int i = 0; i < m; ++i) {
-                const int t = REV ? m - 1 - i : i;
-                const float x = vs[t][cc], d = al[t];
+    auto first = [&](int u) { return (REV ? tiles - 1 - u : u) * TT; };   // of the u-th tile in order, from the sequence's start
+    IO nk[R], nv[2];   // the next tile's, as loaded
+    float nd = 0.f, ndv[2];
+    auto fetch = [&](int u) {
+        const int t0 = start + first(u), m = end - t0;
 #pragma unroll
-                for (int r = 0; r < R; r += 4) {
-                    const float4 kk = *reinterpret_cast<const float4 *>(&ks[t][(r >> 2) * 32 + part * 4]);
-                    const float w[4] = {kk.x, kk.y, kk.z, kk.w};
+        for (int j = 0; j < R; ++j) {
+            const int i = threadIdx.x + 128 * j, t = i / (8 * R), x = i % (8 * R);
+            nk[j] = t < m && x < p.N ? k[(size_t)(t0 + t) * ks_stride + x] : from_f32<IO>(0.f);
+        }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[r + e] = REV ? d * fmaf(w[e], x, s[r + e]) : fmaf(w[e], x, d * s[r + e]);
-                }
+        for (int j = 0; j < 2; ++j) {
+            const int i = threadIdx.x + 128 * j, t = i >> 4, c = cb * 16 + (i & 15);
+            nv[j] = from_f32<IO>(0.f);
+            ndv[j] = 1.f;
+            if (t < m && c < p.P) {
+                nv[j] = v[(size_t)(t0 + t) * vs_stride + c];
+                if (!REV) ndv[j] = p.dt[(size_t)(t0 + t) * p.H + h];
+            }
+        }
+        if (threadIdx.x < TT) nd = threadIdx.x < m ? p.dt[(size_t)(t0 + threadIdx.x) * p.H + h] : 0.f;
+    };
+    if (tiles > 0) fetch(0);
+    for (int u = 0; u < tiles; ++u) {
+        const int t0 = first(u), m = min(TT, end - start - t0);
+        if (REV ? u == 0 || t0 % QB == QB - TT : t0 % QB == 0) put(states + ((slot0 + t0 / QB) * p.H + h) * p.N * p.P);   // a chunk begins
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int i = threadIdx.x + 128 * j;
+            ks[i / (8 * R)][i % (8 * R)] = to_f32(nk[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) xs[(threadIdx.x + 128 * j) >> 4][threadIdx.x & 15] = ndv[j] * to_f32(nv[j]);
+        if (threadIdx.x < TT) al[threadIdx.x] = expf(nd * a);
+        __syncthreads();
+        if (u + 1 < tiles) fetch(u + 1);
+        for (int i = 0; i < m; ++i) {
+            const int t = REV ? m - 1 - i : i;
+            const float x = xs[t][cc], d = al[t];
+#pragma unroll
+            for (int r = 0; r < R; r += 4) {
+                const float4 kk = *reinterpret_cast<const float4 *>(&ks[t][(r >> 2) * 32 + part * 4]);
+                const float w[4] = {kk.x, kk.y, kk.z, kk.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[r + e] = REV ? d * fmaf(w[e], x, s[r + e]) : fmaf(w[e], x, d * s[r + e]);
             }
         }
     }
