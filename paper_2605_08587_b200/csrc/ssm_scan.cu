@@ -311,6 +311,7 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
     float *m1 = cb + QB * (QB + 1);        // L_ij dt_j (q_i . k_j)
     float *m2 = m1 + QB * (QB + 1);        // L_ij dt_j (do_i . v_j)
     float *rr = m2 + QB * (QB + 1);        // L_ij (q_i . k_j)(do_i . v_j)
+    __shared__ float tS[32][33], tG[32][33];   // 32 x 32 of S and G: read by rows of lanes, which in memory would be a line per lane
     __shared__ double l[QB];
     __shared__ float dts[QB], ei[QB], ej[QB], xs[QB], zs[QB], red[8][2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -401,16 +402,28 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
         }
         {   // dq, dk, and q^T S do
             float z[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int x = lane; x < N; x += 32) {
+            for (int x0 = 0; x0 < N; x0 += 32) {
+                const int x = x0 + lane;
                 float u[4] = {0.f, 0.f, 0.f, 0.f}, w[4] = {0.f, 0.f, 0.f, 0.f}, dq[4] = {0.f, 0.f, 0.f, 0.f}, dk[4] = {0.f, 0.f, 0.f, 0.f};
-                for (int e = 0; e < P; ++e) {
-                    const float ss = S[(size_t)x * P + e], gg = G[(size_t)x * P + e];
+                for (int e0 = 0; e0 < P; e0 += 32) {
+                    const int ne = min(32, P - e0);
+                    __syncthreads();
+                    for (int r = warp; r < 32; r += 8) {
+                        const bool in = x0 + r < N && lane < ne;
+                        tS[r][lane] = in ? S[(size_t)(x0 + r) * P + e0 + lane] : 0.f;
+                        tG[r][lane] = in ? G[(size_t)(x0 + r) * P + e0 + lane] : 0.f;
+                    }
+                    __syncthreads();
+                    for (int e = 0; e < ne; ++e) {
+                        const float ss = tS[lane][e], gg = tG[lane][e];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        u[j] = fmaf(ss, gs[(t0 + j) * P + e], u[j]);
-                        w[j] = fmaf(gg, vs[(t0 + j) * P + e], w[j]);
+                        for (int j = 0; j < 4; ++j) {
+                            u[j] = fmaf(ss, gs[(t0 + j) * P + e0 + e], u[j]);
+                            w[j] = fmaf(gg, vs[(t0 + j) * P + e0 + e], w[j]);
+                        }
                     }
                 }
+                if (x >= N) continue;
                 for (int i = 0; i < m; ++i) {
                     const float qq = qs[i * N + x], kk = ks[i * N + x];
 #pragma unroll
