@@ -294,7 +294,7 @@ template <typename IO>
 __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences seqs, const float *states, const float *dstates, float *part_a, float *part_d)
 {
     extern __shared__ float smem[];
-    const int N = p.N, P = p.P, per = p.H / p.G, g = blockIdx.x % p.G, slot = blockIdx.x / p.G;
+    const int N = p.N, P = p.P, N1 = N + 1, P1 = P + 1 /* rows in shared memory, read across by lanes */, per = p.H / p.G, g = blockIdx.x % p.G, slot = blockIdx.x / p.G;
     int n = 0, hi = p.n_seq;   // the sequence whose first slot is the last one at or before this
     while (hi - n > 1) {
         const int mid = (n + hi) >> 1;
@@ -306,8 +306,8 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
         for (int i = threadIdx.x; i < per; i += 256) part_a[(size_t)slot * p.H + g * per + i] = part_d[(size_t)slot * p.H + g * per + i] = 0.f;
         return;
     }
-    float *qs = smem, *ks = qs + QB * N, *dqs = ks + QB * N, *dks = dqs + QB * N, *vs = dks + QB * N, *gs = vs + QB * P;
-    float *cb = gs + QB * P;               // q_i . k_j             [QB][QB + 1]
+    float *qs = smem, *ks = qs + QB * N1, *dqs = ks + QB * N1, *dks = dqs + QB * N1, *vs = dks + QB * N1, *gs = vs + QB * P1;
+    float *cb = gs + QB * P1;               // q_i . k_j             [QB][QB + 1]
     float *m1 = cb + QB * (QB + 1);        // L_ij dt_j (q_i . k_j)
     float *m2 = m1 + QB * (QB + 1);        // L_ij dt_j (do_i . v_j)
     float *rr = m2 + QB * (QB + 1);        // L_ij (q_i . k_j)(do_i . v_j)
@@ -317,15 +317,15 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int i = tid; i < QB * N; i += 256) {
         const int t = i / N, x = i % N;
-        qs[i] = t < m ? to_f32(static_cast<const IO *>(p.q)[(size_t)(start + t) * p.q_stride + g * N + x]) : 0.f;
-        ks[i] = t < m ? to_f32(static_cast<const IO *>(p.k)[(size_t)(start + t) * p.k_stride + g * N + x]) : 0.f;
-        dqs[i] = dks[i] = 0.f;
+        qs[t * N1 + x] = t < m ? to_f32(static_cast<const IO *>(p.q)[(size_t)(start + t) * p.q_stride + g * N + x]) : 0.f;
+        ks[t * N1 + x] = t < m ? to_f32(static_cast<const IO *>(p.k)[(size_t)(start + t) * p.k_stride + g * N + x]) : 0.f;
+        dqs[t * N1 + x] = dks[t * N1 + x] = 0.f;
     }
     __syncthreads();
     for (int x = tid; x < QB * QB; x += 256) {
         const int i = x / QB, j = x % QB;
         float t = 0.f;
-        for (int e = 0; e < N; ++e) t = fmaf(qs[i * N + e], ks[j * N + e], t);
+        for (int e = 0; e < N; ++e) t = fmaf(qs[i * N1 + e], ks[j * N1 + e], t);
         cb[i * (QB + 1) + j] = t;
     }
     for (int hh = 0; hh < per; ++hh) {
@@ -351,8 +351,8 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
             const int t = i / P, x = i % P;
             const float vv = t < m ? to_f32(static_cast<const IO *>(p.v)[(size_t)(start + t) * p.v_stride + h * P + x]) : 0.f;
             const float go = t < m ? to_f32(static_cast<const IO *>(p.d_out)[((size_t)(start + t) * p.H + h) * P + x]) : 0.f;
-            vs[i] = vv;
-            gs[i] = go;
+            vs[t * P1 + x] = vv;
+            gs[t * P1 + x] = go;
             dd = fmaf(vv, go, dd);
         }
         __syncthreads();
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
             const int i = x / QB, j = x % QB, at = i * (QB + 1) + j;
             float t = 0.f, e = 0.f;
             if (j <= i) {
-                for (int y = 0; y < P; ++y) t = fmaf(gs[i * P + y], vs[j * P + y], t);
+                for (int y = 0; y < P; ++y) t = fmaf(gs[i * P1 + y], vs[j * P1 + y], t);
                 e = expf((float)(l[i] - l[j]));
             }
             m1[at] = j <= i ? e * dts[j] * cb[at] : 0.f;   // (what lies above the diagonal may not be finite)
@@ -378,10 +378,10 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
                 for (int e = 0; e < N; ++e) {
                     const float gg = G[(size_t)e * P + x];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) u[j] = fmaf(ks[(t0 + j) * N + e], gg, u[j]);
+                    for (int j = 0; j < 4; ++j) u[j] = fmaf(ks[(t0 + j) * N1 + e], gg, u[j]);
                 }
                 for (int i = t0; i < m; ++i) {
-                    const float go = gs[i * P + x];
+                    const float go = gs[i * P1 + x];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) w[j] = fmaf(m1[i * (QB + 1) + t0 + j], go, w[j]);
                 }
@@ -389,9 +389,9 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
                 for (int j = 0; j < 4; ++j) {
                     const int t = t0 + j;
                     u[j] *= ej[t];
-                    z[j] = fmaf(u[j], vs[t * P + x], z[j]);
+                    z[j] = fmaf(u[j], vs[t * P1 + x], z[j]);
                     if (t < m)
-                        static_cast<IO *>(p.dv)[((size_t)(start + t) * p.H + h) * P + x] = from_f32<IO>(fmaf(skip, gs[t * P + x], fmaf(dts[t], u[j], w[j])));
+                        static_cast<IO *>(p.dv)[((size_t)(start + t) * p.H + h) * P + x] = from_f32<IO>(fmaf(skip, gs[t * P1 + x], fmaf(dts[t], u[j], w[j])));
                 }
             }
 #pragma unroll
@@ -418,14 +418,14 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
                         const float ss = tS[lane][e], gg = tG[lane][e];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            u[j] = fmaf(ss, gs[(t0 + j) * P + e0 + e], u[j]);
-                            w[j] = fmaf(gg, vs[(t0 + j) * P + e0 + e], w[j]);
+                            u[j] = fmaf(ss, gs[(t0 + j) * P1 + e0 + e], u[j]);
+                            w[j] = fmaf(gg, vs[(t0 + j) * P1 + e0 + e], w[j]);
                         }
                     }
                 }
                 if (x >= N) continue;
                 for (int i = 0; i < m; ++i) {
-                    const float qq = qs[i * N + x], kk = ks[i * N + x];
+                    const float qq = qs[i * N1 + x], kk = ks[i * N1 + x];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         if (i >= t0 + j) dk[j] = fmaf(m2[i * (QB + 1) + t0 + j], qq, dk[j]);
@@ -436,9 +436,9 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
                 for (int j = 0; j < 4; ++j) {
                     const int t = t0 + j;
                     u[j] *= ei[t];
-                    z[j] = fmaf(u[j], qs[t * N + x], z[j]);
-                    dqs[t * N + x] += u[j] + dq[j];
-                    dks[t * N + x] += fmaf(dts[t] * ej[t], w[j], dk[j]);
+                    z[j] = fmaf(u[j], qs[t * N1 + x], z[j]);
+                    dqs[t * N1 + x] += u[j] + dq[j];
+                    dks[t * N1 + x] += fmaf(dts[t] * ej[t], w[j], dk[j]);
                 }
             }
 #pragma unroll
@@ -489,8 +489,8 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
     __syncthreads();
     for (int i = tid; i < m * N; i += 256) {
         const size_t at = ((size_t)(start + i / N) * p.G + g) * N + i % N;
-        static_cast<IO *>(p.dq)[at] = from_f32<IO>(dqs[i]);
-        static_cast<IO *>(p.dk)[at] = from_f32<IO>(dks[i]);
+        static_cast<IO *>(p.dq)[at] = from_f32<IO>(dqs[i / N * N1 + i % N]);
+        static_cast<IO *>(p.dk)[at] = from_f32<IO>(dks[i / N * N1 + i % N]);
     }
 }
 
@@ -582,7 +582,7 @@ static cudaError_t ssm_bwd_t(const SsmParams &p, cudaStream_t stream)
         return cudaGetLastError();
     });
     if (err != cudaSuccess) return err;
-    const size_t smem = ((size_t)QB * (4 * p.N + 2 * p.P) + 4 * QB * (QB + 1)) * sizeof(float);
+    const size_t smem = ((size_t)QB * (4 * (p.N + 1) + 2 * (p.P + 1)) + 4 * QB * (QB + 1)) * sizeof(float);
     err = cudaFuncSetAttribute(ssm_grads_kernel<IO>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (err != cudaSuccess) return err;
     ssm_grads_kernel<IO><<<(unsigned)(slots * p.G), 256, smem, stream>>>(p, seqs, states, dstates, part_a, part_d);
