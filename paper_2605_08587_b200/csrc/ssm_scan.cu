@@ -26,7 +26,8 @@ namespace kla {
 constexpr int TT = 16;   // tokens staged at a time
 
 // Forward.  A warp: 4 columns of the state x 8 parts of its rows, R rows to a thread; a block: 16 columns.  Bound by the latency of one token after another
-// and of a warp's sums over the parts: 8 packed sequences of up to 1024 tokens, 8 heads, N = P = 64, fp32: 129 us (a token at a time, 176).
+// and of a warp's sums over the parts: 8 packed sequences of up to 1024 tokens, 8 heads, N = P = 64, fp32: 78 us (a token at a time 176; four, but
+// with operands converted as they arrive, 129).
 template <typename IO, typename OUT, int R>
 __global__ void __launch_bounds__(128) ssm_scan_kernel(SsmParams p, Sequences seqs)
 {
@@ -287,7 +288,8 @@ __global__ void __launch_bounds__(128) ssm_states_kernel(SsmParams p, Sequences 
     if (REV && p.dinit) put(p.dinit + unit);
 }
 
-// For every N and P and for fp32, on CUDA cores and for that not fast (16 packed sequences of the case that ssm_bwd.cu takes in 454 us: 11.8 ms).
+// For every N and P and for fp32, on CUDA cores and for that not fast (4 x 1024 fp32 tokens of 8 heads, N = P = 64:
+// 332 us; 1 027 with rows a multiple of 32 words apart in shared memory and states read by rows from L1).
 // One block of 256 threads to a chunk and a group; its heads one after another, dq and dk summed in shared memory in that order.
 // A warp owns four tokens of each product, its lanes run along the channels.  da and dd leave as one partial per chunk and head.
 template <typename IO>
