@@ -14,9 +14,9 @@
 // every term carries one rounding like the result's own (with one part of S and G the 2-norm error of dq is 2.7e-3, the rounding alone 1.7e-3).
 // The gradients of dt and a are fp32: their terms come from exact products (DX, k q^T) and from S and G in three bf16 parts (24 bits), summed in fp32.
 //
-// F_t is what is left of sums over rows and columns of R that cancel; da = sum_t dt_t F_t taken from it would add up their rounding.  So da has a sum of its
-// own, sum_{i > j} R_ij (T_i - T_j) with T the sum of dt, from the same sums over 32 tokens, each counted from a point between (or in) its two blocks.
-// (From F: 728 us for 751 on 8 x 4096 tokens, 2-norm errors of da 5e-7, at worst 5e-6, for 3e-7 and 2.4e-6.)
+// F_t is a sum of the terms that span token t and of no others (row sums less column sums come to the same, but a large step's terms would have to cancel in
+// every token before it).  With t in block B of 32 tokens: rows i >= t against columns j of the blocks before B, columns j < t of B against rows of
+// the blocks behind it, and in the diagonal tile sums over i >= t of every j < t, which are sums over columns of sums along rows.
 //
 // 256 threads work, a thread to half a row; one warp issues the products and loads the tiles.  The chain of one slice is what takes the time, not the
 // products (about a third of it) nor memory.  8 x 4096 tokens of 32 heads, N = 128: 751 us, of which the state passes 215; 16 packed sequences of 16
@@ -56,10 +56,8 @@ struct Smem {
     alignas(1024) unsigned char gs[TILE], vs[TILE];       // e^{l_i} do, w_j v
     float a2[2][C], r[2][C], dt[2][C];  // of heads in turn
     // of heads in turn:
-    float rows[2][4][C];      // sums over 32 tokens j of R_ij
-    float acc[2][2][5][C];    // of a token, by half of the columns: its own share of F (but for the sums of rows), z, what ddt has directly, do . v,
-                              // its own share of da
-    float steps[3][4];        // sums of dt over 32 tokens, of three heads in turn
+    float rows[2][4][C];      // sums of R_ij over the 32 tokens j of a block before that of i; in i's own block of R_i'j, i' >= i > j
+    float acc[2][2][5][C];    // of a token, by half of the columns: x, z, what ddt has directly, do . v, its R_ij with tokens i of later blocks
     float tot[2][4];
     float sg[2][8];
     alignas(8) uint64_t bar[B_COUNT];
@@ -78,19 +76,13 @@ struct Params {
 
 // Lanes l and l + 16 get the sum over the warp of w x[l], w the lane's entry of `weights`, through 2 KB of the warp's own: a column of 32 rows to 128 bytes, its
 // 16-byte pieces permuted so that neither the writing of a row nor the reading of a column meets a bank twice.  (By shuffles, 31 with two selections each
-// for 32 columns: 788 us for 735 on 8 x 4096 tokens.)  The lane's own x[diag], where there is one, is left out and returned.
-__device__ __forceinline__ float column_sums(const float (&x)[16], float *own, const float *weights, int diag, float &left_out)
+// for 32 columns: 788 us for 735 on 8 x 4096 tokens.)
+__device__ __forceinline__ float column_sums(const float (&x)[16], float *own, const float *weights)
 {
     const int lane = threadIdx.x & 31, col = lane & 15;
     __syncwarp();
 #pragma unroll
     for (int c = 0; c < 16; ++c) own[c * 32 + (lane ^ (4 * (c & 7)))] = x[c];
-    left_out = 0.f;
-    if ((unsigned)diag < 16) {
-        float &e = own[diag * 32 + (lane ^ (4 * (diag & 7)))];
-        left_out = e;
-        e = 0.f;
-    }
     __syncwarp();
     float s = 0.f;
 #pragma unroll
@@ -158,20 +150,6 @@ struct Head {
     float e;          // e^{l_i}
     float f0, f1;     // decay from this token to the start of block 2 half, 2 half + 1 of the columns (where that lies behind this token's block)
     float whole;      // e^{l_Q}
-    float T;          // sum of dt up to and with this token
-};
-
-// Sums of dt at the ends of the blocks of 32 tokens, and the point that sums over rows of block I and columns of block J <= I are counted from.
-struct Ends {
-    float u[5];
-    __device__ __forceinline__ explicit Ends(const float *steps)
-    {
-        u[0] = 0.f;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) u[b + 1] = u[b] + steps[b];
-    }
-    __device__ __forceinline__ float at(int b) const { return b == 0 ? u[0] : b == 1 ? u[1] : b == 2 ? u[2] : b == 3 ? u[3] : u[4]; }
-    __device__ __forceinline__ float between(int I, int J) const { return 0.5f * (at(I) + at(J + 1)); }
 };
 
 template <int N>
@@ -207,15 +185,7 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         hd.a = next_a;
         hd.dt = next_dt;
         const BlockScan b(hd.dt, hd.a);
-        float T = hd.dt * hd.a * LOG2E < NO_DECAY ? 0.f : hd.dt;   // (nothing is carried across a token that wipes the state)
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const float u = __shfl_up_sync(0xffffffffu, T, o);
-            if (lane >= o) T += u;
-        }
-        float *tot = sm.tot[i & 1], *steps = sm.steps[i % 3];
-        if (half == 0 && lane == 31) steps[warp] = T;
-        __syncwarp();
+        float *tot = sm.tot[i & 1];
         if (lane == 0) {
             if (half == 0) tot[warp] = b.tot;
             mbar_arrive(&sm.bar[B_TOT]);
@@ -232,11 +202,10 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         hd.f0 = exp2f(b.rest + (half == 0 ? 0.f : warp == 0 ? t1 : 0.f));
         hd.f1 = exp2f(b.rest + (half == 0 ? 0.f : warp == 0 ? t1 + t2 : warp == 1 ? t2 : 0.f));
         hd.whole = exp2f(t0 + t1 + t2 + t3);
-        hd.T = Ends(steps).at(warp) + T;
         return true;
     };
     // Gradients of dt and a of the i-th head, a thread of the first half to a token; of the other blocks' tokens it needs the sums.
-    auto finish = [&](int i, float a, float dt, float whole, float T) {
+    auto finish = [&](int i, float a, float dt, float whole) {
         if (!wait(B_E, i)) return false;
         if (half) return true;
         const int h = wk.h0 + i;
@@ -251,11 +220,12 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
             if (b >= warp) {
                 o = acc[0][0][at] + acc[1][0][at];
 #pragma unroll
-                for (int J = 0; J <= b; ++J) o += sm.rows[i & 1][J][at];
+                for (int J = 0; J < b; ++J)
+                    if (J < warp) o += sm.rows[i & 1][J][at];
             }
             if (b <= warp) y = acc[0][1][at] + acc[1][1][at];
             if (b > warp) later += o;
-            if (b == warp) own = o, zt = y;
+            if (b == warp) own = o, zt = y + (acc[0][4][at] + acc[1][4][at]);
             if (b < warp) earlier += y;
         }
         float suffix = own, prefix = zt, d = acc[0][3][t] + acc[1][3][t];
@@ -268,15 +238,9 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
             earlier += __shfl_xor_sync(0xffffffffu, earlier, o);
         }
         const float before = __shfl_up_sync(0xffffffffu, prefix, 1);
-        // (a decay that is zero has no gradient, where the sums leave the rounding of what cancels in them)
-        const float F = dt * a * LOG2E < NO_DECAY ? 0.f : suffix + later + (lane ? before : 0.f) + earlier + whole * all;
+        const float F = sm.rows[i & 1][warp][t] + suffix + later + (lane ? before : 0.f) + earlier + whole * all;
         if (in) p.a.ddt[row_out * p.a.H + h] = fmaf(a, F, acc[0][2][t] + acc[1][2][t]);
-        const Ends ends(sm.steps[i % 3]);
-        float da = acc[0][4][t] + acc[1][4][t] + (t == 0 ? whole * all * ends.at(4) : 0.f);
-#pragma unroll
-        for (int J = 0; J < 4; ++J)
-            if (J <= warp) da = fmaf(sm.rows[i & 1][J][t], T - ends.between(warp, J), da);
-        if (!in) da = 0.f;
+        float da = in ? dt * F : 0.f;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             da += __shfl_xor_sync(0xffffffffu, da, o);
@@ -289,8 +253,8 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         return true;
     };
     Head hd, next;
-    float c0 = 0.f, c1 = 0.f, diag = 0.f, z = 0.f, x = 0.f, dd = 0.f, sg = 0.f;   // sums over a head's slices (c: of R without dt, by block of columns)
-    float old_a = 0.f, old_dt = 0.f, old_whole = 0.f, old_T = 0.f;    // of the head before
+    float near = 0.f, far = 0.f, z = 0.f, x = 0.f, dd = 0.f, sg = 0.f;   // sums over a head's slices (near, far: of R without dt, in the token's block and behind)
+    float old_a = 0.f, old_dt = 0.f, old_whole = 0.f;    // of the head before
     bool ok = decays(0, hd) && wait(B_CB, 0);
 #pragma unroll 1
     for (int it = 0; ok && it < wk.items; ++it) {
@@ -356,8 +320,9 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
 #pragma unroll
         for (int ii = 0; ii < 2; ++ii) {
             const int I = 2 * half + ii;   // block of 32 columns i
+            float behind = 0.f;            // in the diagonal tile: the row's sum from a column on
 #pragma unroll
-            for (int u = 0; u < 32; u += 16) {
+            for (int u = 16; u >= 0; u -= 16) {
                 float2 mm[8];
                 float rs[16], row = 0.f;
                 if (I < warp) {
@@ -397,16 +362,23 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
                     *piece(sm.m[half], t, ii * 4 + (u >> 3) + y) = make_uint4(pack2(mm[4 * y]), pack2(mm[4 * y + 1]), pack2(mm[4 * y + 2]), pack2(mm[4 * y + 3]));
-                if (ii == 1 && u == 16) {
+                if (ii == 1 && u == 0) {
                     fence_async_smem();
                     tc_fence_before();
                     mbar_arrive(&sm.bar[B_M]);
                 }
                 if (I >= warp) {   // (the scaled do has been read by its product)
-                    float tt;   // R_tt is in none of the sums: it belongs to ddt alone
-                    const float s = column_sums(rs, reinterpret_cast<float *>(sm.gs) + (warp * 2 + half) * 512, &sm.dt[i & 1][warp * 32], I == warp ? lane - u : -1, tt);
-                    diag += tt;
-                    (ii ? c1 : c0) += row - tt;
+                    if (I == warp) {
+#pragma unroll
+                        for (int y = 15; y >= 0; --y) {
+                            behind += rs[y];
+                            rs[y] = u + y > lane ? behind : 0.f;
+                        }
+                        if (u == 0) near += behind;   // (R_tt among it)
+                    } else {
+                        far += row;
+                    }
+                    const float s = column_sums(rs, reinterpret_cast<float *>(sm.gs) + (warp * 2 + half) * 512, &sm.dt[i & 1][warp * 32]);
                     if (lane < 16) {
                         float &to = sm.rows[i & 1][warp][I * 32 + u + lane];
                         to = sl ? to + s : s;
@@ -418,7 +390,7 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         // -- the next head's decays and the last one's gradients, while M do and k G are formed
         const bool last = sl == slices - 1;
         if (last && i + 1 < heads && !(ok = decays(i + 1, next))) break;
-        if (last && i > 0 && !(ok = finish(i - 1, old_a, old_dt, old_whole, old_T))) break;
+        if (last && i > 0 && !(ok = finish(i - 1, old_a, old_dt, old_whole))) break;
         // -- dv and z
         if (!(ok = wait(B_C2, it))) break;
         tc_fence_after();
@@ -459,13 +431,10 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         }
         __syncwarp();
         if (last) {
-            const Ends ends(sm.steps[i % 3]);
-            const float c_all = c0 + c1, zt = hd.w * z;
-            sm.acc[i & 1][half][0][t] = x - hd.dt * c_all;
-            sm.acc[i & 1][half][1][t] = zt;
-            sm.acc[i & 1][half][4][t] = x * hd.T + zt * (ends.at(4) - hd.T) -
-                                        hd.dt * (c0 * (hd.T - ends.between(2 * half, warp)) + c1 * (hd.T - ends.between(2 * half + 1, warp)));
-            sm.acc[i & 1][half][2][t] = fmaf(hd.wn, z, c_all + diag);
+            sm.acc[i & 1][half][0][t] = x;
+            sm.acc[i & 1][half][1][t] = hd.w * z;
+            sm.acc[i & 1][half][2][t] = fmaf(hd.wn, z, near + far);
+            sm.acc[i & 1][half][4][t] = hd.dt * far;
             sm.acc[i & 1][half][3][t] = dd;
             for (int o = 16; o > 0; o >>= 1) sg += __shfl_xor_sync(0xffffffffu, sg, o);
             if (lane == 0) sm.sg[i & 1][threadIdx.x >> 5] = sg;
@@ -473,12 +442,11 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
             old_a = hd.a;
             old_dt = hd.dt;
             old_whole = hd.whole;
-            old_T = hd.T;
             hd = next;
-            c0 = c1 = diag = z = x = dd = sg = 0.f;
+            near = far = z = x = dd = sg = 0.f;
         }
     }
-    ok = ok && finish(heads - 1, old_a, old_dt, old_whole, old_T);
+    ok = ok && finish(heads - 1, old_a, old_dt, old_whole);
     if (!ok || sm.abort_flag) return;
     // -- the heads' sum as an operand, row j
 #pragma unroll

@@ -31,7 +31,8 @@ def check_gradients(g, s, dy, df, lens, N, P):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("step", [1.0, 15.0, 1e3, 1e6])
-@pytest.mark.parametrize("N, P, dtype, flags", [(64, 64, BF, KLA_FLAG_FORCE_SIMT), (128, 64, F32, KLA_FLAG_NONE), (24, 16, F32, KLA_FLAG_NONE), (96, 40, BF, KLA_FLAG_NONE)])
+@pytest.mark.parametrize("N, P, dtype, flags", [(64, 64, BF, KLA_FLAG_NONE), (128, 64, BF, KLA_FLAG_NONE), (64, 128, BF, KLA_FLAG_NONE),
+                                                (64, 64, BF, KLA_FLAG_FORCE_SIMT), (128, 64, F32, KLA_FLAG_NONE), (24, 16, F32, KLA_FLAG_NONE), (96, 40, BF, KLA_FLAG_NONE)])
 def test_gradients_beside_large_steps(N, P, dtype, flags, step):
     """At most one large step to 32 tokens; every token's gradients, those before such a step among them."""
     lens, H, G = [200, 90], 4, 2
