@@ -579,6 +579,8 @@ cudaError_t launch_ssm_sums(const float *part_a, const float *part_d, int n, int
     return cudaGetLastError();
 }
 
+static size_t grads_smem(int N, int P) { return ((size_t)QB * (4 * (N + 1) + 2 * (P + 1)) + 4 * QB * (QB + 1)) * sizeof(float); }
+
 template <typename IO>
 static cudaError_t ssm_bwd_t(const SsmParams &p, cudaStream_t stream)
 {
@@ -593,10 +595,10 @@ static cudaError_t ssm_bwd_t(const SsmParams &p, cudaStream_t stream)
         return cudaGetLastError();
     });
     if (err != cudaSuccess) return err;
-    const size_t smem = ((size_t)QB * (4 * (p.N + 1) + 2 * (p.P + 1)) + 4 * QB * (QB + 1)) * sizeof(float);
-    err = cudaFuncSetAttribute(ssm_grads_kernel<IO>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // (the limit is the function's, not the call's: always that of the largest widths, so that a call on another host thread finds it high enough)
+    err = cudaFuncSetAttribute(ssm_grads_kernel<IO>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)grads_smem(256, 256));
     if (err != cudaSuccess) return err;
-    ssm_grads_kernel<IO><<<(unsigned)(slots * p.G), 256, smem, stream>>>(p, seqs, states, dstates, part_a, part_d);
+    ssm_grads_kernel<IO><<<(unsigned)(slots * p.G), 256, grads_smem(p.N, p.P), stream>>>(p, seqs, states, dstates, part_a, part_d);
     count_launch(1);
     return launch_ssm_sums(part_a, part_d, (int)slots, p.H, p.da, p.dd, stream);
 }
