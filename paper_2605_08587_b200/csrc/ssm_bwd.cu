@@ -54,7 +54,7 @@ struct Smem {
     alignas(1024) unsigned char sp[3][TILE];              // parts of S, then of G: [row of N][64 columns]
     alignas(1024) unsigned char m[2][TILE];               // M^T, at the end the sum over heads: [64 of i][j][64]
     alignas(1024) unsigned char gs[TILE], vs[TILE];       // e^{l_i} do, w_j v
-    float a2[2][C], r[2][C], dt[2][C];  // of heads in turn
+    float a2[2][C], lo[2][C], r[2][C], dt[2][C];  // of heads in turn
     // of heads in turn:
     float rows[2][4][C];      // sums of R_ij over the 32 tokens j of a block before that of i; in i's own block of R_i'j, i' >= i > j
     float acc[2][2][5][C];    // of a token, by half of the columns: x, z, what ddt has directly, do . v, its R_ij with tokens i of later blocks
@@ -145,7 +145,7 @@ __device__ __forceinline__ void tmem_ld16x2(uint32_t ta, uint32_t tb, float (&a)
 
 // A head's scalars of one token.
 struct Head {
-    float dt, a, a2;
+    float dt, a, a2, lo;
     float w, wn;      // dt_j e^{l_Q - l_j}, and without dt_j
     float e;          // e^{l_i}
     float f0, f1;     // decay from this token to the start of block 2 half, 2 half + 1 of the columns (where that lies behind this token's block)
@@ -184,15 +184,16 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
     auto decays = [&](int i, Head &hd) {   // of the i-th head
         hd.a = next_a;
         hd.dt = next_dt;
-        const BlockScan b(hd.dt, hd.a);
+        const BlockScan<true> b(hd.dt, hd.a);
         float *tot = sm.tot[i & 1];
         if (lane == 0) {
             if (half == 0) tot[warp] = b.tot;
             mbar_arrive(&sm.bar[B_TOT]);
         }
         hd.a2 = b.a2;
+        hd.lo = b.lo;
         const float r = exp2f(b.a2);
-        if (half == 0) sm.a2[i & 1][t] = b.a2;
+        if (half == 0) sm.a2[i & 1][t] = b.a2, sm.lo[i & 1][t] = b.lo;
         else sm.r[i & 1][t] = r, sm.dt[i & 1][t] = hd.dt;
         if (!wait(B_TOT, i)) return false;
         const float t0 = tot[0], t1 = tot[1], t2 = tot[2], t3 = tot[3];
@@ -316,7 +317,7 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         // -- M, the sum over heads, and the sums of R
         if (!(ok = wait(B_DX, it))) break;
         tc_fence_after();
-        const float *rr_ = sm.r[i & 1], *aa = sm.a2[i & 1];
+        const float *rr_ = sm.r[i & 1], *aa = sm.a2[i & 1], *ll = sm.lo[i & 1];
 #pragma unroll
         for (int ii = 0; ii < 2; ++ii) {
             const int I = 2 * half + ii;   // block of 32 columns i
@@ -341,9 +342,10 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
                             L[0] = mul2(f2(ri.x, ri.y), f);
                             L[1] = mul2(f2(ri.z, ri.w), f);
                         } else {
-                            const float4 ai = load4(aa + I * 32 + u + y);
-                            L[0] = f2(u + y >= lane ? ex2_approx(ai.x - hd.a2) : 0.f, u + y + 1 >= lane ? ex2_approx(ai.y - hd.a2) : 0.f);
-                            L[1] = f2(u + y + 2 >= lane ? ex2_approx(ai.z - hd.a2) : 0.f, u + y + 3 >= lane ? ex2_approx(ai.w - hd.a2) : 0.f);
+                            const float4 ai = load4(aa + I * 32 + u + y), li = load4(ll + I * 32 + u + y);
+                            auto decay = [&](int i, float hi, float lo) { return u + y + i >= lane ? ex2_approx((hi - hd.a2) + (lo - hd.lo)) : 0.f; };
+                            L[0] = f2(decay(0, ai.x, li.x), decay(1, ai.y, li.y));
+                            L[1] = f2(decay(2, ai.z, li.z), decay(3, ai.w, li.w));
                         }
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {

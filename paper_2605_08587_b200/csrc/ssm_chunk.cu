@@ -130,13 +130,13 @@ __device__ void decay_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
     for (int c = 0; c < wk.chunks; ++c) {
         const int next = (c + 1) * C + t;
         const float next_dt = next < wk.len ? dtp[(size_t)next * p.a.H] : 0.f;
-        const BlockScan b(dt, a);
+        const BlockScan<true> b(dt, a);
         float *tot = sm.tot[c & 1];   // (of chunk c - 2: read before that chunk's P was written)
         if (lane == 0) {
             tot[warp] = b.tot;
             mbar_arrive(&sm.bar[B_TOT]);
         }
-        const float r = exp2f(b.a2), cf = dt * exp2f(b.rest);
+        const float cf = dt * exp2f(b.rest), whole = rintf(b.a2), f = (b.a2 - whole) + b.lo, dtf = dt * exp2f(-f);
         if (!bar_wait(&sm.bar[B_TOT], c, &sm.abort_flag)) break;
         const float t1 = tot[1], t2 = tot[2], t3 = tot[3];
         const float w = cf * exp2f(warp == 0 ? t1 + t2 + t3 : warp == 1 ? t2 + t3 : warp == 2 ? t3 : 0.f);
@@ -144,10 +144,10 @@ __device__ void decay_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
         sm.weight[t] = w;
         warp_arrive(&sm.bar[B_W]);
         if (c > 0 && !bar_wait(&sm.bar[B_P], c - 1, &sm.abort_flag)) break;     // and its scalars
-        sm.sc.a2[t] = b.a2;
-        sm.sc.r[t] = r;
+        sm.sc.nn[t] = -whole;
+        sm.sc.f[t] = f;
         sm.sc.cf[t] = cf;
-        sm.sc.dt[t] = dt;
+        sm.sc.dtf[t] = dtf;
         warp_arrive(&sm.bar[B_SCAL]);
         dt = next_dt;
     }
@@ -244,7 +244,7 @@ __device__ void output_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
     auto scores = [&](int c, float &e, uint4 (&x)[4]) {
         const int st = c % STAGES;
         if (!bar_wait(&sm.bar[B_SCAL], c, &sm.abort_flag)) return false;
-        const float a2 = sm.sc.a2[t], r = sm.sc.r[t];
+        const float whole = -sm.sc.nn[t], frac = sm.sc.f[t], r = exp2f(whole + frac);
         const float *tot = sm.tot[c & 1];
         const float t0 = tot[0], t1 = tot[1], t2 = tot[2];
         // decay from the chunk's start to this row, and from block J's end to it
@@ -257,8 +257,8 @@ __device__ void output_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
 #pragma unroll 1
         for (int jj = 0; jj < 2; ++jj) {
             const int J = 2 * half + jj;   // block of 32 columns
-            const float2 f = f2(jj ? f1 : f0), ai = f2(a2);
-            const float *cfs = &sm.sc.cf[J * 32], *as = &sm.sc.a2[J * 32], *ds = &sm.sc.dt[J * 32];
+            const float2 f = f2(jj ? f1 : f0), ni = f2(whole), fi = f2(frac);
+            const float *cfs = &sm.sc.cf[J * 32], *ns = &sm.sc.nn[J * 32], *ds = &sm.sc.dtf[J * 32];
 #pragma unroll
             for (int i = 0; i < 32; i += 16) {
                 float2 y[8];
@@ -278,8 +278,8 @@ __device__ void output_role(Smem<PARTS> &sm, const Params &p, const Work &wk)
                     } else {
 #pragma unroll
                         for (int u = 0; u < 8; u += 2) {
-                            const float4 aj = load4(as + i + 2 * u), dj = load4(ds + i + 2 * u);
-                            const float2 l0 = add2(ai, f2(-aj.x, -aj.y)), l1 = add2(ai, f2(-aj.z, -aj.w));
+                            const float4 nj = load4(ns + i + 2 * u), dj = load4(ds + i + 2 * u);
+                            const float2 l0 = add2(add2(ni, f2(nj.x, nj.y)), fi), l1 = add2(add2(ni, f2(nj.z, nj.w)), fi);
                             y[u] = mul2(mul2(f2(v[2 * u], v[2 * u + 1]), f2(dj.x, dj.y)), f2(ex2_approx(l0.x), ex2_approx(l0.y)));
                             y[u + 1] = mul2(mul2(f2(v[2 * u + 2], v[2 * u + 3]), f2(dj.z, dj.w)), f2(ex2_approx(l1.x), ex2_approx(l1.y)));
                         }

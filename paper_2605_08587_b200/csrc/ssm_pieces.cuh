@@ -167,29 +167,40 @@ constexpr int STATE_ELEMS = 128 * NS;
 
 // Scalars of a chunk, a thread to a token.  Sums of log2 decays run inside blocks of 32 tokens (a warp): decays between tokens of a block are
 // exponentials of differences of short sums; those from a token to its block's end come from a sum of their own, so that they are accurate
-// however far the block's start lies back.
-//   a2 inclusive sum inside the block
-//   r = 2^a2 (from the block's start);  cf = dt 2^(sum of what follows in the block)
-// A token's log2 decay below NO_DECAY counts as that (its power of two is zero in fp32 all the same): a token that wipes the state would otherwise leave
-// sums whose differences have lost the digits of the tokens behind it.
-constexpr float NO_DECAY = -152.f;
+// however far the block's start lies back.  Sums whose differences count carry their rounding errors in a second float: behind tokens that decay strongly
+// they are large, and the decay between two ordinary ones there would have only the digits that one float leaves (sums of 3 000: 2^-13).
+//   a2 + lo inclusive sum inside the block
+//   cf = dt 2^(sum of what follows in the block)
+//   nn = -n, f: a2 + lo = n + f with n whole;  dtf = dt 2^-f.  L_ij dt_j = 2^(n_i - n_j + f_i) dtf_j, where n_i - n_j is exact
+// A token's log2 decay below NO_DECAY counts as that (its power of two is zero in fp32 all the same), however large its step: sums stay below 2^15, where
+// two floats hold them to 2^-33.
+constexpr float NO_DECAY = -1024.f;
 struct alignas(16) Scalars {
-    float a2[C], r[C], cf[C], dt[C];
+    float nn[C], f[C], cf[C], dtf[C];
 };
+template <bool DIFFERENCES>   // whether differences of a2 are taken (else lo is zero)
 struct BlockScan {
-    float a2, rest, tot;   // inclusive sum, what follows to the block's end, the whole block
+    float a2, lo, rest, tot;   // inclusive sum, what follows to the block's end, the whole block
     __device__ __forceinline__ BlockScan(float dt, float a)
     {
         const int lane = threadIdx.x & 31;
         const float l = dt * a * LOG2E, x = l < NO_DECAY ? NO_DECAY : l;   // (NaN stays)
-        float up = x, down = x;
+        float up = x, err = 0.f, down = x;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const float t = __shfl_up_sync(0xffffffffu, up, o), u = __shfl_down_sync(0xffffffffu, down, o);
-            if (lane >= o) up += t;
+            if constexpr (DIFFERENCES) {
+                const float te = __shfl_up_sync(0xffffffffu, err, o);
+                const float sum = up + t, b = sum - up, e = (up - (sum - b)) + (t - b);   // sum + e = up + t
+                if (lane >= o) err += te + e;
+                if (lane >= o) up = sum;
+            } else {
+                if (lane >= o) up += t;
+            }
             if (lane + o < 32) down += u;
         }
         a2 = up;
+        lo = err;
         const float behind = __shfl_down_sync(0xffffffffu, down, 1);
         rest = lane < 31 ? behind : 0.f;
         tot = __shfl_sync(0xffffffffu, down, 0);

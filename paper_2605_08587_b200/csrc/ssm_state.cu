@@ -71,7 +71,7 @@ __device__ void work(Smem &sm, const Params &p, const Piece &pc, int h, int sl, 
     const size_t out_step = (size_t)p.a.H * (p.a.P / NS) * STATE_ELEMS;
     // This token's weight in the cx-th chunk, and the chunk's decay
     auto decays = [&](int cx, float &w, float &gamma) {
-        const BlockScan b(dt, a);
+        const BlockScan<false> b(dt, a);
         float *tot = sm.tot[cx & 1];   // (of two chunks before: read before the last one's product)
         if (lane == 0) {
             if (half == 0) tot[warp] = b.tot;

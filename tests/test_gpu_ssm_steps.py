@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from layer_refs import check, grads
-from paper_2605_08587_b200 import KLA_FLAG_FORCE_SIMT, KLA_FLAG_NONE, kla_ssm_bwd
+from paper_2605_08587_b200 import KLA_FLAG_FORCE_SIMT, KLA_FLAG_NONE, kla_ssm_bwd, kla_ssm_fwd
 from test_gpu_ssm import BF, F32, make, reference, rel_of
 
 
@@ -39,3 +39,22 @@ def test_gradients_beside_large_steps(N, P, dtype, flags, step):
     s, seqs, dy, df = make(lens, H, G, N, P, dtype, seed=3)
     s["dt"][0, [5, 40, 64, 127, 128, 199, 200, 250]] = step
     check_gradients(backward(s, seqs, dy, df, flags), s, dy, df, lens, N, P)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("step", [8.0, 1e6, 1e30])
+@pytest.mark.parametrize("N, P, dtype, flags", [(64, 64, BF, KLA_FLAG_NONE), (128, 64, BF, KLA_FLAG_NONE)])
+def test_runs_of_tokens_that_wipe_the_state(N, P, dtype, flags, step):
+    """Up to 24 of 32 tokens decay by exp(-8) and more each (and write nothing: their keys are zero); the decays between the ordinary ones behind them keep
+    their digits."""
+    lens, H, G = [200, 90], 4, 2
+    s, seqs, dy, df = make(lens, H, G, N, P, dtype, seed=3)
+    at = [*range(3, 19), 64, 65, *range(70, 94), *range(130, 140), 199, 200, 201, 250]
+    s["dt"][0, at] = step
+    s["k"][0, at] = 0
+    y, fin = kla_ssm_fwd(**s, **seqs, out_dtype=F32, flags=flags)
+    g = backward(s, seqs, dy, df, flags)
+    _, (ry, rf), _, (my, mf) = reference(s, lens)
+    check(y[0], ry, my, rel_of(lens, N, P), "out")
+    check(fin, rf, mf, 2.0 ** -17 + (max(lens) + 64) * 2.0 ** -24, "final_state")
+    check_gradients(g, s, dy, df, lens, N, P)
