@@ -338,6 +338,7 @@ __global__ void __launch_bounds__(256) ssm_grads_kernel(SsmParams p, Sequences s
         if (warp == 0) {   // sums of log decays, in 64 bits: their differences are what counts
             const float d = lane < m ? p.dt[(size_t)(start + lane) * p.H + h] : 0.f;
             double s = (double)d * (double)a;
+            if (s < -1e4) s = -1e4;   // (zero in fp32 all the same; a larger one would take the others' digits from the sums)
             for (int o = 1; o < 32; o <<= 1) {
                 const double t = __shfl_up_sync(0xffffffffu, s, o);
                 if (lane >= o) s += t;

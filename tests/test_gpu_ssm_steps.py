@@ -43,7 +43,7 @@ def test_gradients_beside_large_steps(N, P, dtype, flags, step):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("step", [8.0, 1e6, 1e30])
-@pytest.mark.parametrize("N, P, dtype, flags", [(64, 64, BF, KLA_FLAG_NONE), (128, 64, BF, KLA_FLAG_NONE)])
+@pytest.mark.parametrize("N, P, dtype, flags", [(64, 64, BF, KLA_FLAG_NONE), (128, 64, BF, KLA_FLAG_NONE), (64, 64, BF, KLA_FLAG_FORCE_SIMT), (24, 16, F32, KLA_FLAG_NONE)])
 def test_runs_of_tokens_that_wipe_the_state(N, P, dtype, flags, step):
     """Up to 24 of 32 tokens decay by exp(-8) and more each (and write nothing: their keys are zero); the decays between the ordinary ones behind them keep
     their digits."""
