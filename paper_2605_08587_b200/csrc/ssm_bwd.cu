@@ -449,7 +449,7 @@ __device__ void workers(Smem &sm, const Params &p, const Work &wk)
         }
     }
     ok = ok && finish(heads - 1, old_a, old_dt, old_whole);
-    if (!ok || sm.abort_flag) return;
+    if (!__all_sync(0xffffffffu, ok && !sm.abort_flag)) return;   // (a warp leaves as one: the wait below is a vote)
     // -- the heads' sum as an operand, row j
 #pragma unroll
     for (int i = 0; i < 8; ++i)
