@@ -308,6 +308,8 @@ def test_states_in_place(lens, H, N, P):
     assert fin2.data_ptr() == state.data_ptr() and torch.equal(y, y2) and torch.equal(state, fin)
 
 
+# (At these sizes every (chunk, group) is one block's: heads are shared among blocks only where there are fewer than half as many as SMs, see
+# test_gpu_ssm_shares.py.)
 @pytest.mark.gpu
 @pytest.mark.parametrize("H, G, N, P", [(4, 2, 64, 64), (6, 2, 128, 64)])
 def test_backward_of_more_chunks_than_blocks_run_at_once(H, G, N, P):
