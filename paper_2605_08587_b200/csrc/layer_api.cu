@@ -132,7 +132,7 @@ static kla_status norm_args(const kla_desc *d, int32_t width, int32_t group, con
     if (!(eps >= 0.f) || !std::isfinite(eps)) return KLA_ERR_EPS;
     if (width < 1 || group < 1 || width % group || x_stride < width) return KLA_ERR_SHAPE;
     if (gate && (residual || gate_stride < width)) return KLA_ERR_SHAPE;
-    if (scale && !residual) return KLA_ERR_SHAPE;
+    if (scale && !residual && rows) return KLA_ERR_SHAPE;   // (without rows the residual has no address)
     if (residual && residual_dtype != KLA_F32 && residual_dtype != d->io_dtype) return KLA_ERR_DTYPE;
     if (rows * (width / group) >= (int64_t)1 << 31) return KLA_ERR_SHAPE;
     if (!aligned({x, residual, gate}) || !aligned4({scale, weight})) return KLA_ERR_ALIGN;
@@ -342,7 +342,7 @@ kla_status kla_norm_bwd(const kla_desc *desc, int32_t width, int32_t group, cons
     p.d_residual_out = residual ? d_residual_out : nullptr;
     p.dx = dx;
     p.dresidual = dresidual;
-    p.dscale = residual ? dscale : nullptr;
+    p.dscale = residual || !p.rows ? dscale : nullptr;
     p.dgate = dgate;
     p.dweight = dweight;
     p.partial = static_cast<float *>(desc->workspace);

@@ -389,7 +389,8 @@ static bool whole_rows(const NormParams &p, int io_dtype)
     const int bytes = io_dtype == KLA_BF16 ? 2 : 4;
     return (size_t)p.x_stride * bytes % 16 == 0 && (!p.gate || (size_t)p.gate_stride * bytes % 16 == 0);
 }
-static int norm_mode(const NormParams &p) { return p.residual ? NORM_ADD : p.gate ? (p.gate_first ? NORM_GATE_FIRST : NORM_GATE) : NORM_PLAIN; }
+// (without rows a residual may be null, and the sums over rows are wanted all the same)
+static int norm_mode(const NormParams &p) { return p.residual || p.dscale ? NORM_ADD : p.gate ? (p.gate_first ? NORM_GATE_FIRST : NORM_GATE) : NORM_PLAIN; }
 
 // Blocks of the backward's persistent grid (each leaves one partial), and the row runs of the column sums of any width.
 static int bwd_blocks(int rows, const NormShape &s)
