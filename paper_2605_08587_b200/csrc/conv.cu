@@ -6,9 +6,11 @@
 // Backward, with g_t = dy_t act'(p_t):   dx_t = sum_i w[i] g_{t+W-1-i} (tokens of the same sequence), plus the final state's gradient
 // for the last W - 1 tokens;  dw[c][i] = sum_t g_t x_{t-W+1+i};  db = sum_t g_t.
 //
-// 8 x 4096 tokens of 2304 channels, 4 taps, bf16: 82 us, 3.7 TB/s (46 us by its bytes); backward of 16 packed sequences, 363 MB: 123 us.  Bound by the issue
-// of instructions: W multiply-adds, an exponential and a reciprocal per value (the latter two alone take 34 us of 75 M values).  A thread owns
-// four neighbouring channels as two pairs (packed arithmetic) and walks a run of tokens with the window in registers, so a value is loaded
+// 8 x 4096 tokens of 2304 channels, 4 taps, bf16: 82 us, 3.7 TB/s (46 us by its bytes); backward of 16 packed sequences, 363 MB: 123 us.  Forward: bound by
+// the wait for loads, of which three blocks of 80 registers hold too few in flight (instructions issue in 43 % of the cycles, 7 of 12 stalled warps of
+// an issue wait for memory; the exponential and the reciprocal of a value keep their unit 45 % busy, 34 us of 75 M values).  Backward: by the latency of
+// arithmetic on four warps per scheduler (issue 55 %, 0.5 waiting for memory); its SMs work 79 % of the time (594 blocks for 592 places of two rounds).
+// A thread owns four neighbouring channels as two pairs (packed arithmetic) and walks a run of tokens with the window in registers, so a value is loaded
 // once, but for the W - 1 before (backward: and behind) its run; eight rows (backward: four) are in flight while the last ones are worked on.
 // Rows between a sequence's border and a run's end take a loop of their own, so that the others' code is straight.
 #include "layer_ops.h"

@@ -19,8 +19,8 @@
 // the blocks behind it, and in the diagonal tile sums over i >= t of every j < t, which are sums over columns of sums along rows.
 //
 // 256 threads work, a thread to half a row; one warp issues the products and loads the tiles.  The chain of one slice is what takes the time, not the
-// products (about a third of it) nor memory.  8 x 4096 tokens of 32 heads, N = 128: 751 us, of which the state passes 215; 16 packed sequences of 16
-// heads, N = 64: 475 us.  512 workers with a quarter of a row spill (975-995 us for 796 then), a warpgroup of its own for the scalars waits for the
+// products (about a third of it) nor memory.  8 x 4096 tokens of 32 heads, N = 128: 755 us, of which the state passes 215; 16 packed sequences of 16
+// heads, N = 64: 467 us.  512 workers with a quarter of a row spill (975-995 us for 796 then), a warpgroup of its own for the scalars waits for the
 // workers as they for it (831), k G beside the 128 x 128 work where N = 64 leaves tensor memory for it takes the same time.
 #include "ssm_pieces.cuh"
 

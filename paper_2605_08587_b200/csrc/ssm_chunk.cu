@@ -24,8 +24,9 @@
 // Decays are products of exponentials of sums that do not exceed zero (for a < 0): inside a block of 32 tokens one exponential per
 // element, between blocks the product of a factor per row, one per pair of blocks and one per column, which costs two multiplications.
 //
-// What bounds it: the port of the shared memory.  Of the 4 900 cycles of a chunk at N = 128 the products' operands take 1 920, the loads' tiles 640, and the
-// roles' own reads and writes 2 300 (counted).  P of the next chunk formed before the outputs of the last, with P and q S there twice and k once,
+// What bounds it: the port of the shared memory.  A working SM takes 5 200 cycles for a chunk at N = 128, of which by count the products' operands take 1 920,
+// the loads' tiles 640, and the roles' own reads and writes 2 300.  (On 8 x 4096 tokens of 32 heads, 200 us, the SMs work 83 % of the time: 256 blocks
+// on 148 SMs.)  P of the next chunk formed before the outputs of the last, with P and q S there twice and k once,
 // 209 us for 201 on 8 x 4096 tokens of 32 heads (k comes too late); what helped last were accesses: one arrival per warp at a barrier and outputs staged without
 // bank conflicts (201 -> 196).
 //

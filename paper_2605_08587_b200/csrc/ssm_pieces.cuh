@@ -64,7 +64,7 @@ struct Parts {
     float *decay;        // [n_seq n][H]: the whole part's decay
     // Cut where the blocks of whole sequences would leave more than half the SMs without work and it pays: a chunk takes about 2.6 us in the
     // output kernel and 1.5 in the pass over the states before it, which also costs two launches, 8 us.  (65 536 tokens, H8 d 128: whole
-    // 1 295 us, in nine parts 309; 777 tokens of 32 heads: whole 25 us, in four parts 29.)
+    // 1 295 us, in nine parts 305; 777 tokens of 32 heads: whole 25 us, in four parts 29.)
     Parts(const SsmParams &a, int sms, void *workspace) : n(1), seg_len(0), state(nullptr), decay(nullptr)
     {
         int longest = a.T;

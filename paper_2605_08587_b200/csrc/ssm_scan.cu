@@ -288,8 +288,8 @@ __global__ void __launch_bounds__(128) ssm_states_kernel(SsmParams p, Sequences 
     if (REV && p.dinit) put(p.dinit + unit);
 }
 
-// For every N and P and for fp32, on CUDA cores and for that not fast (4 x 1024 fp32 tokens of 8 heads, N = P = 64:
-// 332 us; 1 027 with rows a multiple of 32 words apart in shared memory and states read by rows from L1).
+// For every N and P and for fp32, on CUDA cores and for that not fast (4 x 1024 fp32 tokens of 8 heads in as many groups, N = P = 64:
+// 339 us; a case of that size took 332 for 1 027 with rows a multiple of 32 words apart in shared memory and states read by rows from L1).
 // One block of 256 threads to a chunk and a group; its heads one after another, dq and dk summed in shared memory in that order.
 // A warp owns four tokens of each product, its lanes run along the channels.  da and dd leave as one partial per chunk and head.
 template <typename IO>
